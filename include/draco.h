@@ -268,6 +268,62 @@ int draco_generate(float* out, int rows, int64_t len, int row0, float mean, floa
 int draco_corrupt(const draco_plan* plan, void* R, const int* adv_idx, const int* adv_model,
                   const float* adv_param, int n_adv, uint64_t seed, void* stream);
 
+/*
+ * Lists of tensors.  A model's gradients and parameters are many tensors of several types; the code works on flat fp32 vectors.
+ * These calls stand between the two: norms and clipping of a list, a list packed into a row of G for draco_encode, and the decoded
+ * sum applied to a list of parameters.  (The paper has no counterpart: its model is one vector.)
+ *
+ * A layout holds the sizes and types of one list, the split of the work, and scratch for partial sums (8 bytes a warp, at most 300 KB,
+ * and 60 bytes a tensor).  Tensor t takes entries off_t .. off_t + numel[t] - 1 of the flat vector, off_t = numel[0] + .. + numel[t-1];
+ * d = their sum (draco_layout_size).  Each call takes the list as a host array of device addresses, read before the call returns.
+ * Tensors are dense (numel contiguous elements); an address needs the alignment of its element only.  NULL: the tensor is absent (a
+ * parameter without a gradient).  Sizes of zero are allowed.  The rows of G are such a list too.
+ *
+ * Norms: DRACO_NORM_2, sqrt(sum g^2), or DRACO_NORM_MAX, max |g|, over all tensors that are present; sums in fp64, results rounded to fp32.
+ * Clipping: factor c = max_norm / norm where norm > max_norm, else 1 (max_norm >= 0; INFINITY: no clipping).  A norm that is not
+ * finite in fp32 bounds nothing: draco_clip and draco_pack then use c = 1, and draco_update leaves everything as it was.
+ *
+ * Calls on one layout must not overlap on the device (they share its scratch).  The layout's device must be the current one
+ * (DRACO_EINVAL otherwise).  Results do not depend on timing: the same inputs give the same bits.
+ */
+typedef struct draco_layout draco_layout;
+enum { DRACO_F32 = 0, DRACO_BF16 = 1, DRACO_F16 = 2 };
+enum { DRACO_NORM_2 = 0, DRACO_NORM_MAX = 1 };
+#define DRACO_MAX_TENSORS 65536
+
+/* numel, type: host arrays of `count` entries.  DRACO_ELIMIT: more than DRACO_MAX_TENSORS tensors. */
+int draco_layout_create(int count, const int64_t* numel /*host*/, const int* type /*host*/, draco_layout** out);
+int draco_layout_destroy(draco_layout* layout);
+int64_t draco_layout_size(const draco_layout* layout);
+
+/* norm: device [1] fp32, the norm of all; each: device [count] fp32, the norm of every tensor (0 where absent), or NULL. */
+int draco_norm(draco_layout* layout, const void* const* tensors /*host*/, int kind, float* norm, float* each, void* stream);
+
+/*
+ * out_t = c tensor_t (fp32 product, rounded once to the tensor's type), c from the norm of all tensors, or of tensor t alone
+ * (separately != 0).  out: host array of device addresses, or NULL: in place (nothing is written where c = 1).  out_t is tensor_t or
+ * shares no memory with any tensor; an address twice among the outputs, or an output at another tensor's address, is DRACO_EINVAL, and
+ * so is an output for an absent tensor or none for one that is there.
+ * norm: device [1] fp32, the norm of all before clipping; each: device [count], only with separately; both may be NULL.
+ */
+int draco_clip(draco_layout* layout, const void* const* tensors /*host*/, void* const* out /*host*/, int kind, float max_norm, int separately,
+               float* norm, float* each, void* stream);
+
+/* row[off_t + i] = c tensor_t[i] in fp32, zeros for absent tensors.  row: device [d] fp32, 4-byte aligned (a row of G), sharing no
+ * memory with the tensors (DRACO_EINVAL).  norm: device [1] fp32, as in draco_clip, or NULL (with max_norm = INFINITY no norm is formed). */
+int draco_pack(draco_layout* layout, const void* const* tensors /*host*/, int kind, float max_norm, float* row, float* norm, void* stream);
+
+/*
+ * The update of draco_decode_update for a list of parameters, from a decoded sum u with its norm bounded:
+ * w_t[i] <- w_t[i] - (scale c) u[off_t + i], c from the norm of u (all d entries), one fused multiply-add in fp32, rounded once to
+ * w_t's type.  master: device [d] fp32 or NULL; with it master[k] <- master[k] - (scale c) u[k] and w_t takes the rounded master.
+ * The entries of absent parameters are left alone, in master too.  u and master: 16-byte aligned; they, and the parameters, share no
+ * memory with each other (DRACO_EINVAL, also for an address twice in the list).  norm: device [1] fp32, the norm of u, or NULL; with
+ * neither norm nor a finite max_norm u is read once and whatever it holds is applied.
+ */
+int draco_update(draco_layout* layout, void* const* params /*host*/, const float* u, float* master, int kind, float max_norm, float scale,
+                 float* norm, void* stream);
+
 const char* draco_strerror(int code);
 /* Text of the last CUDA error seen by this library on the calling thread ("" if none). */
 const char* draco_last_cuda_error(void);

@@ -17,6 +17,9 @@ REP, CYC, CYC_PACKED = 0, 1, 2
 ADV_REVGRAD, ADV_CONST, ADV_GAUSS = 0, 1, 2
 OK, EINVAL, ECUDA, ETOOMANY, ENOMEM, EINTERNAL, ELIMIT, ENOMAJ, EUNSURE = 0, -1, -2, -3, -4, -5, -6, 1, 2
 MAX_N = 128
+F32, BF16, F16 = 0, 1, 2
+NORM_2, NORM_MAX = 0, 1
+MAX_TENSORS = 65536
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 
@@ -49,6 +52,8 @@ def _load() -> C.CDLL:
 
 lib = _load()
 
+_TYPES = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16}
+
 _vp, _i, _i64, _u64, _f = C.c_void_p, C.c_int, C.c_int64, C.c_uint64, C.c_float
 _SIGS = {
     "draco_plan_create": ([_i, _i, _i64, _i, C.POINTER(_vp)], _i),
@@ -73,6 +78,13 @@ _SIGS = {
                              C.POINTER(DracoInfo)], _i),
     "draco_generate": ([_vp, _i, _i64, _i, _f, _f, _u64, _vp], _i),
     "draco_corrupt": ([_vp, _vp, C.POINTER(_i), C.POINTER(_i), C.POINTER(_f), _i, _u64, _vp], _i),
+    "draco_layout_create": ([_i, C.POINTER(_i64), C.POINTER(_i), C.POINTER(_vp)], _i),
+    "draco_layout_destroy": ([_vp], _i),
+    "draco_layout_size": ([_vp], _i64),
+    "draco_norm": ([_vp, C.POINTER(_vp), _i, _vp, _vp, _vp], _i),
+    "draco_clip": ([_vp, C.POINTER(_vp), C.POINTER(_vp), _i, _f, _i, _vp, _vp, _vp], _i),
+    "draco_pack": ([_vp, C.POINTER(_vp), _i, _f, _vp, _vp, _vp], _i),
+    "draco_update": ([_vp, C.POINTER(_vp), _vp, _vp, _i, _f, _f, _vp, _vp], _i),
     "draco_strerror": ([_i], C.c_char_p),
     "draco_last_cuda_error": ([], C.c_char_p),
 }
@@ -280,3 +292,110 @@ class Plan:
                                        adv_seed & 0xFFFFFFFFFFFFFFFF, _ptr(Z), _ptr(u_host), _ptr(flags_host),
                                        C.byref(out)))
         return out.as_dict()
+
+
+def _dense(t) -> bool:
+    """Whether the tensor's elements fill one piece of memory, in whatever order."""
+    if t.is_contiguous():
+        return True
+    run = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != run:
+            return False
+        run *= size
+    return True
+
+
+class Layout:
+    """draco_layout: sizes and types of a list of tensors, on the current device.
+
+    ``numels``: the numbers of elements.  ``types``: F32, BF16, F16 or torch's dtypes, one for each tensor or one for all.  The calls
+    take the list itself: tensors of these sizes and types on the layout's device, None for one that is absent, or raw addresses.
+    ``norm`` and ``clip`` take tensors that are dense in any order of their dimensions; ``pack`` and ``update``, whose flat vectors
+    follow the order of the elements, contiguous ones.
+    """
+
+    def __init__(self, numels, types):
+        import torch
+        self.numels = [int(n) for n in numels]
+        one = isinstance(types, int) or str(types) in _TYPES
+        self.types = [self._type(t) for t in ([types] * len(self.numels) if one else types)]
+        if len(self.types) != len(self.numels):
+            raise DracoError(f"{len(self.numels)} sizes, {len(self.types)} types")
+        count = len(self.numels)
+        h = _vp()
+        _check(lib.draco_layout_create(count, (_i64 * count)(*self.numels), (_i * count)(*self.types), C.byref(h)))
+        self._h = h
+        self.device = torch.cuda.current_device()
+        self.d = lib.draco_layout_size(h)
+
+    @classmethod
+    def of(cls, tensors):
+        """The layout of these tensors."""
+        tensors = list(tensors)
+        return cls([t.numel() for t in tensors], [t.dtype for t in tensors])
+
+    @staticmethod
+    def _type(t):
+        if isinstance(t, int):
+            return t
+        if str(t) not in _TYPES:
+            raise DracoError(f"{t}: tensors are float32, bfloat16 or float16")
+        return _TYPES[str(t)]
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib.draco_layout_destroy(self._h)
+            self._h = None
+
+    __del__ = close
+
+    def _here(self, x, numel, type_, what, ordered=True):
+        """Address of a tensor of this size and type on the layout's device; ints and None as in the other calls."""
+        if x is None or isinstance(x, int):
+            return x
+        if x.numel() != numel or _TYPES.get(str(x.dtype)) != type_:
+            raise DracoError(f"{what}: {x.numel()} x {x.dtype}, not {numel} of type {type_}")
+        if not x.is_cuda or x.get_device() != self.device:
+            raise DracoError(f"{what} is on {x.device}, not on cuda:{self.device}")
+        if not (x.is_contiguous() if ordered else _dense(x)):
+            raise DracoError(f"{what} is not {'contiguous' if ordered else 'dense'}: strides {x.stride()}")
+        return x.data_ptr()
+
+    def _list(self, tensors, what, ordered):
+        if len(tensors) != len(self.numels):
+            raise DracoError(f"{what}: {len(tensors)} tensors, not {len(self.numels)}")
+        a = (_vp * len(tensors))()
+        for i, (x, n, t) in enumerate(zip(tensors, self.numels, self.types)):
+            a[i] = self._here(x, n, t, f"{what}[{i}]", ordered)
+        return a
+
+    def norm(self, tensors, norm, each=None, kind: int = NORM_2, stream=None):
+        """draco_norm: norm <- the norm of all tensors, each[t] <- that of tensor t."""
+        return _check(lib.draco_norm(self._h, self._list(tensors, "tensors", False), kind, self._here(norm, 1, F32, "norm"),
+                                     self._here(each, len(self.numels), F32, "each"), _stream(stream)))
+
+    def clip(self, tensors, max_norm: float, out=None, norm=None, each=None, separately: bool = False, kind: int = NORM_2, stream=None):
+        """draco_clip: the tensors scaled so that their norm (separately: that of each) is at most max_norm, in place or to ``out``.
+
+        An ``out`` tensor has the memory order of its input."""
+        src = self._list(tensors, "tensors", False)
+        dst = None
+        if out is not None:
+            dst = self._list(out, "out", False)
+            for i, (x, y) in enumerate(zip(tensors, out)):
+                if hasattr(x, "stride") and hasattr(y, "stride") and (x.shape != y.shape or x.stride() != y.stride()):
+                    raise DracoError(f"out[{i}]: shape {tuple(y.shape)}, strides {y.stride()}, not {tuple(x.shape)}, {x.stride()}")
+        return _check(lib.draco_clip(self._h, src, dst, kind, max_norm, bool(separately), self._here(norm, 1, F32, "norm"),
+                                     self._here(each, len(self.numels), F32, "each"), _stream(stream)))
+
+    def pack(self, tensors, row, max_norm: float = float("inf"), norm=None, kind: int = NORM_2, stream=None):
+        """draco_pack: the tensors one after the other in the fp32 row, clipped."""
+        return _check(lib.draco_pack(self._h, self._list(tensors, "tensors", True), kind, max_norm, self._here(row, self.d, F32, "row"),
+                                     self._here(norm, 1, F32, "norm"), _stream(stream)))
+
+    def update(self, params, u, scale: float, max_norm: float = float("inf"), master=None, norm=None, kind: int = NORM_2, stream=None):
+        """draco_update: params <- params - scale * c * u, by way of the fp32 master copy where there is one."""
+        return _check(lib.draco_update(self._h, self._list(params, "params", True), self._here(u, self.d, F32, "u"),
+                                       self._here(master, self.d, F32, "master"), kind, max_norm, scale, self._here(norm, 1, F32, "norm"),
+                                       _stream(stream)))

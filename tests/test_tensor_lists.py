@@ -1,0 +1,64 @@
+"""Lists of tensors: what is refused before anything runs (no compute: this runs without a GPU)."""
+import ctypes
+
+import pytest
+
+
+def _binding():
+    from paper_1803_09877_b200 import build
+    build.build()
+    from paper_1803_09877_b200 import binding
+    return binding
+
+
+@pytest.mark.parametrize("numels,types", [([], []), ([4, -1], [0, 0]), ([4], [3]), ([4], [-1]), ([1 << 49], [0]), ([1 << 48, 1 << 48, 1], [0, 1, 2])])
+def test_layouts_that_are_refused(numels, types):
+    b = _binding()
+    h = ctypes.c_void_p(7)
+    n = len(numels)
+    rc = b.lib.draco_layout_create(n, (ctypes.c_int64 * max(n, 1))(*numels), (ctypes.c_int * max(n, 1))(*types), ctypes.byref(h))
+    assert rc == b.EINVAL and not h.value
+
+
+def test_too_many_tensors():
+    b = _binding()
+    n = b.MAX_TENSORS + 1
+    h = ctypes.c_void_p()
+    assert b.lib.draco_layout_create(n, (ctypes.c_int64 * n)(), (ctypes.c_int * n)(), ctypes.byref(h)) == b.ELIMIT
+
+
+def test_null_arguments():
+    b = _binding()
+    lib, h = b.lib, ctypes.c_void_p()
+    one, zero = (ctypes.c_int64 * 1)(4), (ctypes.c_int * 1)(0)
+    assert lib.draco_layout_create(1, one, zero, None) == b.EINVAL
+    assert lib.draco_layout_create(1, None, zero, ctypes.byref(h)) == b.EINVAL
+    assert lib.draco_layout_create(1, one, None, ctypes.byref(h)) == b.EINVAL
+    assert lib.draco_layout_size(None) == b.EINVAL
+    assert lib.draco_layout_destroy(None) == b.OK
+    tensors = (ctypes.c_void_p * 1)(4096)
+    assert lib.draco_norm(None, tensors, 0, 4096, None, None) == b.EINVAL
+    assert lib.draco_clip(None, tensors, None, 0, 1.0, 0, None, None, None) == b.EINVAL
+    assert lib.draco_pack(None, tensors, 0, 1.0, 4096, None, None) == b.EINVAL
+    assert lib.draco_update(None, tensors, 4096, None, 0, 1.0, 1.0, None, None) == b.EINVAL
+
+
+def test_python_refuses_sizes_and_types_that_do_not_go_together():
+    b = _binding()
+    import torch
+    with pytest.raises(b.DracoError, match="2 sizes, 1 types"):
+        b.Layout([1, 2], [b.F32])
+    with pytest.raises(b.DracoError, match="float64"):
+        b.Layout([1], [torch.float64])
+    with pytest.raises(b.DracoError, match="float64"):
+        b.Layout.of([torch.zeros(3, dtype=torch.float64)])
+
+
+def test_dense_tensors():
+    """Elements that fill one piece of memory in whatever order: their sum of squares does not depend on it."""
+    b = _binding()
+    import torch
+    x = torch.zeros(4, 6, 5)
+    assert b._dense(x) and b._dense(x.permute(2, 0, 1)) and b._dense(torch.zeros(2, 3, 4, 5).to(memory_format=torch.channels_last))
+    assert b._dense(x[1]) and b._dense(x[:, :1, :1][:1]) and b._dense(torch.zeros(0, 3))
+    assert not b._dense(x[:, :, ::2]) and not b._dense(x[:, 1:]) and not b._dense(torch.zeros(3, 1).expand(3, 4)) and not b._dense(x[:, :1, :1])
