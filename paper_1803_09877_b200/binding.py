@@ -164,7 +164,17 @@ class _CtypesCalls:
         return _check(lib.draco_locate_decode(plan, _ptr(R), _ptr(f), _ptr(flags), _ptr(u), _stream(stream)))
 
     @staticmethod
+    def norm(*_):                       # binding.py itself lists the addresses then
+        return NotImplemented
+
+    clip = pack = update = norm
+
+    @staticmethod
     def set_current_stream(raw, device):
+        pass
+
+    @staticmethod
+    def set_exchange(tensor, parameter, capsule):
         pass
 
 
@@ -294,6 +304,29 @@ class Plan:
         return out.as_dict()
 
 
+class _Meta(C.Structure):
+    """What the native calls compare a list of tensors with."""
+    _fields_ = [("count", _i64), ("d", _i64), ("numels", C.POINTER(_i64)), ("types", C.POINTER(C.c_int32)), ("device", C.c_int32)]
+
+
+_exchange_known = False
+
+
+def _find_exchange(torch):
+    """torch's table of DLPack functions, where it offers one, for the native calls."""
+    global _exchange_known
+    if not _exchange_known:
+        _exchange_known = True
+        capsule = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+        if capsule is not None:
+            _native.set_exchange(torch.Tensor, torch.nn.Parameter, capsule)
+
+
+def _order(t) -> list:
+    """Sizes and strides, those of sizes of one apart, which say nothing."""
+    return [(n, st if n != 1 else 0) for n, st in zip(t.shape, t.stride())]
+
+
 def _dense(t) -> bool:
     """Whether the tensor's elements fill one piece of memory, in whatever order."""
     if t.is_contiguous():
@@ -326,8 +359,12 @@ class Layout:
         h = _vp()
         _check(lib.draco_layout_create(count, (_i64 * count)(*self.numels), (_i * count)(*self.types), C.byref(h)))
         self._h = h
+        self._address = h.value
         self.device = torch.cuda.current_device()
         self.d = lib.draco_layout_size(h)
+        self._meta = _Meta(count, self.d, (_i64 * count)(*self.numels), (C.c_int32 * count)(*self.types), self.device)
+        self._meta_address = C.addressof(self._meta)
+        _find_exchange(torch)
 
     @classmethod
     def of(cls, tensors):
@@ -347,6 +384,7 @@ class Layout:
         if getattr(self, "_h", None):
             lib.draco_layout_destroy(self._h)
             self._h = None
+            self._address = None
 
     __del__ = close
 
@@ -372,6 +410,9 @@ class Layout:
 
     def norm(self, tensors, norm, each=None, kind: int = NORM_2, stream=None):
         """draco_norm: norm <- the norm of all tensors, each[t] <- that of tensor t."""
+        rc = _native.norm(self._address, self._meta_address, tensors, norm, each, kind, stream)
+        if rc is not NotImplemented:
+            return rc
         return _check(lib.draco_norm(self._h, self._list(tensors, "tensors", False), kind, self._here(norm, 1, F32, "norm"),
                                      self._here(each, len(self.numels), F32, "each"), _stream(stream)))
 
@@ -379,23 +420,32 @@ class Layout:
         """draco_clip: the tensors scaled so that their norm (separately: that of each) is at most max_norm, in place or to ``out``.
 
         An ``out`` tensor has the memory order of its input."""
+        rc = _native.clip(self._address, self._meta_address, tensors, max_norm, out, norm, each, separately, kind, stream)
+        if rc is not NotImplemented:
+            return rc
         src = self._list(tensors, "tensors", False)
         dst = None
         if out is not None:
             dst = self._list(out, "out", False)
             for i, (x, y) in enumerate(zip(tensors, out)):
-                if hasattr(x, "stride") and hasattr(y, "stride") and (x.shape != y.shape or x.stride() != y.stride()):
+                if hasattr(x, "stride") and hasattr(y, "stride") and _order(x) != _order(y):
                     raise DracoError(f"out[{i}]: shape {tuple(y.shape)}, strides {y.stride()}, not {tuple(x.shape)}, {x.stride()}")
         return _check(lib.draco_clip(self._h, src, dst, kind, max_norm, bool(separately), self._here(norm, 1, F32, "norm"),
                                      self._here(each, len(self.numels), F32, "each"), _stream(stream)))
 
     def pack(self, tensors, row, max_norm: float = float("inf"), norm=None, kind: int = NORM_2, stream=None):
         """draco_pack: the tensors one after the other in the fp32 row, clipped."""
+        rc = _native.pack(self._address, self._meta_address, tensors, row, max_norm, norm, kind, stream)
+        if rc is not NotImplemented:
+            return rc
         return _check(lib.draco_pack(self._h, self._list(tensors, "tensors", True), kind, max_norm, self._here(row, self.d, F32, "row"),
                                      self._here(norm, 1, F32, "norm"), _stream(stream)))
 
     def update(self, params, u, scale: float, max_norm: float = float("inf"), master=None, norm=None, kind: int = NORM_2, stream=None):
         """draco_update: params <- params - scale * c * u, by way of the fp32 master copy where there is one."""
+        rc = _native.update(self._address, self._meta_address, params, u, scale, max_norm, master, norm, kind, stream)
+        if rc is not NotImplemented:
+            return rc
         return _check(lib.draco_update(self._h, self._list(params, "params", True), self._here(u, self.d, F32, "u"),
                                        self._here(master, self.d, F32, "master"), kind, max_norm, scale, self._here(norm, 1, F32, "norm"),
                                        _stream(stream)))

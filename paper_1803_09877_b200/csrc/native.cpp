@@ -110,6 +110,229 @@ PyObject* locate_decode(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     Py_END_ALLOW_THREADS return status(rc);
 }
 
+// ---- lists of tensors ----
+
+// DLPack's C interface (the public header's structures), by which torch hands out a tensor's address, type, sizes and device in one call:
+// 56 ns a tensor, where the five attributes cost 370.  A list that is not plain tensors of the layout's sizes and types on its device is
+// left to binding.py (NotImplemented), which takes what is unusual and names what is wrong.
+struct DLDevice {
+    int32_t type, id;
+};
+struct DLDataType {
+    uint8_t code, bits;
+    uint16_t lanes;
+};
+struct DLTensor {
+    void* data;
+    DLDevice device;
+    int32_t ndim;
+    DLDataType dtype;
+    int64_t *shape, *strides;
+    uint64_t byte_offset;
+};
+struct DLPackExchangeAPI {
+    uint32_t major, minor;
+    void *previous, *allocator, *from_object, *to_object;
+    int (*tensor_from_object)(void* object, DLTensor* out);
+    void* current_work_stream;
+};
+
+const DLPackExchangeAPI* g_exchange = nullptr;
+PyObject *g_tensor = nullptr, *g_parameter = nullptr;       // torch.Tensor and torch.nn.Parameter; their subclasses are left to binding.py
+
+struct Meta {                                               // binding.py's _Meta
+    int64_t count, d;
+    const int64_t* numels;
+    const int32_t* types;
+    int32_t device;
+};
+
+// Whether the elements fill one piece of memory: in the order of the dimensions, or (ordered false) in any.
+bool dense(const DLTensor& t, bool ordered) {
+    constexpr int kMost = 8;
+    if (t.ndim > kMost) return false;
+    int64_t run = 1;
+    bool contiguous = true;
+    for (int k = t.ndim - 1; k >= 0; --k) {
+        if (t.shape[k] == 1) continue;
+        if (t.strides && t.strides[k] != run) contiguous = false;
+        run *= t.shape[k];
+    }
+    if (contiguous || run == 0) return true;
+    if (ordered) return false;
+    bool done[kMost] = {};
+    run = 1;
+    for (int n = 0; n < t.ndim; ++n) {
+        int next = -1;
+        for (int k = 0; k < t.ndim; ++k)
+            if (!done[k] && t.shape[k] != 1 && t.strides[k] == run) next = k;
+        if (next < 0) break;
+        done[next] = true;
+        run *= t.shape[next];
+    }
+    for (int k = 0; k < t.ndim; ++k)
+        if (!done[k] && t.shape[k] != 1) return false;
+    return true;
+}
+
+// The tensor as the layout has it, or false, without an error.
+bool as_told(PyObject* x, int64_t numel, int type, int device, bool ordered, DLTensor* t) {
+    if (!g_exchange || ((PyObject*)Py_TYPE(x) != g_tensor && (PyObject*)Py_TYPE(x) != g_parameter)) return false;
+    if (g_exchange->tensor_from_object(x, t) != 0) {
+        PyErr_Clear();
+        return false;
+    }
+    static const DLDataType types[] = {{2, 32, 1}, {4, 16, 1}, {2, 16, 1}};       // DRACO_F32, DRACO_BF16, DRACO_F16
+    constexpr int kCuda = 2;
+    if (type < 0 || type > 2 || t->device.type != kCuda || t->device.id != device || t->dtype.code != types[type].code ||
+        t->dtype.bits != types[type].bits || t->dtype.lanes != 1)
+        return false;
+    int64_t n = 1;
+    for (int k = 0; k < t->ndim; ++k) n *= t->shape[k];
+    return n == numel && dense(*t, ordered);
+}
+
+// Address of an fp32 vector of n elements, an int or None.
+bool vector_address(PyObject* x, const Meta* m, int64_t n, void** out) {
+    if (x == Py_None || PyLong_Check(x)) return address(x, out);
+    DLTensor t;
+    if (!as_told(x, n, DRACO_F32, m->device, true, &t)) return false;
+    *out = static_cast<char*>(t.data) + t.byte_offset;
+    return true;
+}
+
+struct Addresses {
+    void* few[512];
+    void** p = few;
+    ~Addresses() {
+        if (p != few) PyMem_Free(p);
+    }
+    // beside: a list whose tensors have the same sizes and strides
+    bool take(PyObject* list, const Meta* m, bool ordered, PyObject* beside = nullptr) {
+        if (!PyList_Check(list) && !PyTuple_Check(list)) return false;
+        if (PySequence_Fast_GET_SIZE(list) != m->count) return false;
+        if (m->count > (int64_t)(sizeof(few) / sizeof(few[0]))) {
+            p = static_cast<void**>(PyMem_Malloc(sizeof(void*) * m->count));
+            if (!p) {
+                p = few;
+                return false;
+            }
+        }
+        PyObject** items = PySequence_Fast_ITEMS(list);
+        for (int64_t i = 0; i < m->count; ++i) {
+            PyObject* x = items[i];
+            p[i] = nullptr;
+            if (x == Py_None) continue;
+            DLTensor t, b;
+            if (!as_told(x, m->numels[i], m->types[i], m->device, ordered, &t)) return false;
+            if (beside) {
+                PyObject* y = PySequence_Fast_ITEMS(beside)[i];
+                if (y == Py_None || g_exchange->tensor_from_object(y, &b) != 0) {
+                    PyErr_Clear();
+                    return false;
+                }
+                if (t.ndim != b.ndim) return false;
+                for (int k = 0; k < t.ndim; ++k)
+                    if (t.shape[k] != b.shape[k] || (t.shape[k] != 1 && t.strides[k] != b.strides[k])) return false;
+            }
+            p[i] = static_cast<char*>(t.data) + t.byte_offset;
+        }
+        return true;
+    }
+};
+
+#define LAYOUT reinterpret_cast<draco_layout*>(layout)
+#define META const Meta* m = static_cast<const Meta*>(meta)
+
+bool layout_of(PyObject* const* args, Py_ssize_t nargs, Py_ssize_t want, void** layout, void** meta) {
+    if (nargs != want) {
+        PyErr_Format(PyExc_TypeError, "%zd arguments, not %zd", want, nargs);
+        return false;
+    }
+    return address(args[0], layout) && address(args[1], meta);
+}
+
+bool number(PyObject* x, float* out) {
+    *out = (float)PyFloat_AsDouble(x);
+    return !PyErr_Occurred();
+}
+
+bool whole(PyObject* x, int* out) {
+    const long v = PyLong_AsLong(x);
+    *out = v < INT32_MIN || v > INT32_MAX ? -1 : (int)v;
+    return !PyErr_Occurred();
+}
+
+PyObject* left_to_python() {
+    if (PyErr_Occurred()) return nullptr;
+    Py_RETURN_NOTIMPLEMENTED;
+}
+
+// (layout, meta, tensors, norm, each, kind, stream)
+PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    void *layout, *meta, *norm, *each, *st;
+    int kind;
+    if (!layout_of(args, nargs, 7, &layout, &meta)) return nullptr;
+    META;
+    Addresses a;
+    if (!a.take(args[2], m, false) || !vector_address(args[3], m, 1, &norm) || !vector_address(args[4], m, m->count, &each)) return left_to_python();
+    if (!whole(args[5], &kind) || !stream_of(args[6], &st)) return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS rc = draco_norm(LAYOUT, a.p, kind, (float*)norm, (float*)each, st);
+    Py_END_ALLOW_THREADS return status(rc);
+}
+
+// (layout, meta, tensors, max_norm, out, norm, each, separately, kind, stream)
+PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    void *layout, *meta, *norm, *each, *st;
+    int kind;
+    float max_norm;
+    if (!layout_of(args, nargs, 10, &layout, &meta)) return nullptr;
+    META;
+    Addresses a, b;
+    const bool out = args[4] != Py_None;
+    if (!a.take(args[2], m, false) || (out && !b.take(args[4], m, false, args[2])) || !vector_address(args[5], m, 1, &norm) ||
+        !vector_address(args[6], m, m->count, &each))
+        return left_to_python();
+    const int separately = PyObject_IsTrue(args[7]);
+    if (separately < 0 || !number(args[3], &max_norm) || !whole(args[8], &kind) || !stream_of(args[9], &st)) return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS rc = draco_clip(LAYOUT, a.p, out ? b.p : nullptr, kind, max_norm, separately, (float*)norm, (float*)each, st);
+    Py_END_ALLOW_THREADS return status(rc);
+}
+
+// (layout, meta, tensors, row, max_norm, norm, kind, stream)
+PyObject* pack(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    void *layout, *meta, *row, *norm, *st;
+    int kind;
+    float max_norm;
+    if (!layout_of(args, nargs, 8, &layout, &meta)) return nullptr;
+    META;
+    Addresses a;
+    if (!a.take(args[2], m, true) || !vector_address(args[3], m, m->d, &row) || !vector_address(args[5], m, 1, &norm)) return left_to_python();
+    if (!number(args[4], &max_norm) || !whole(args[6], &kind) || !stream_of(args[7], &st)) return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS rc = draco_pack(LAYOUT, a.p, kind, max_norm, (float*)row, (float*)norm, st);
+    Py_END_ALLOW_THREADS return status(rc);
+}
+
+// (layout, meta, params, u, scale, max_norm, master, norm, kind, stream)
+PyObject* update(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    void *layout, *meta, *u, *master, *norm, *st;
+    int kind;
+    float scale, max_norm;
+    if (!layout_of(args, nargs, 10, &layout, &meta)) return nullptr;
+    META;
+    Addresses a;
+    if (!a.take(args[2], m, true) || !vector_address(args[3], m, m->d, &u) || !vector_address(args[6], m, m->d, &master) ||
+        !vector_address(args[7], m, 1, &norm))
+        return left_to_python();
+    if (!number(args[4], &scale) || !number(args[5], &max_norm) || !whole(args[8], &kind) || !stream_of(args[9], &st)) return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS rc = draco_update(LAYOUT, a.p, (const float*)u, (float*)master, kind, max_norm, scale, (float*)norm, st);
+    Py_END_ALLOW_THREADS return status(rc);
+}
+
 void keep(PyObject*& slot, PyObject* value) {
     Py_INCREF(value);
     Py_XSETREF(slot, value);
@@ -131,8 +354,22 @@ PyObject* set_current_stream(PyObject*, PyObject* args) {     // (raw, device)
     Py_RETURN_NONE;
 }
 
+PyObject* set_exchange(PyObject*, PyObject* args) {           // (torch.Tensor, torch.nn.Parameter, its DLPack exchange capsule)
+    PyObject *tensor, *parameter, *capsule;
+    if (!PyArg_ParseTuple(args, "OOO", &tensor, &parameter, &capsule)) return nullptr;
+    const auto* api = static_cast<const DLPackExchangeAPI*>(PyCapsule_GetPointer(capsule, "dlpack_exchange_api"));
+    if (!api) return nullptr;
+    if (api->major == 1 && api->tensor_from_object) {
+        keep(g_tensor, tensor);
+        keep(g_parameter, parameter);
+        g_exchange = api;
+    }
+    Py_RETURN_NONE;
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(encode), FAST(locate), FAST(decode), FAST(decode_update), FAST(locate_decode),
+                         FAST(norm), FAST(clip), FAST(pack), FAST(update), {"set_exchange", set_exchange, METH_VARARGS, nullptr},
                          {"set_functions", set_functions, METH_VARARGS, nullptr},
                          {"set_current_stream", set_current_stream, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
