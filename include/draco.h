@@ -291,7 +291,8 @@ enum { DRACO_F32 = 0, DRACO_BF16 = 1, DRACO_F16 = 2 };
 enum { DRACO_NORM_2 = 0, DRACO_NORM_MAX = 1 };
 #define DRACO_MAX_TENSORS 65536
 
-/* numel, type: host arrays of `count` entries.  DRACO_ELIMIT: more than DRACO_MAX_TENSORS tensors. */
+/* numel, type: host arrays of `count` entries.  DRACO_ELIMIT: more than DRACO_MAX_TENSORS tensors or 2^40
+ * elements. */
 int draco_layout_create(int count, const int64_t* numel /*host*/, const int* type /*host*/, draco_layout** out);
 int draco_layout_destroy(draco_layout* layout);
 int64_t draco_layout_size(const draco_layout* layout);

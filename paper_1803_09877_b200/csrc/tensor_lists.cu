@@ -5,8 +5,8 @@
 //
 // All of them stream the list once or twice and are bound by HBM; short ones by the latency of one or two launches.
 //
-// Split.  A list is cut into items of 4 KB (of the tensor's own type), which start on 16-byte boundaries of the tensor's memory, wherever
-// the tensor starts, and the items are dealt to the warps of the grid in contiguous ranges of equal length, so that a tensor of any size costs
+// Split.  A list is cut into lines of one word a lane, which begin on word boundaries of the tensor's memory, wherever the tensor
+// begins, and the lines are dealt to the warps of the grid in contiguous ranges of equal length, so that a tensor of any size costs
 // what it holds.  The ranges depend on sizes alone and are made once, with the layout; the tensors' addresses come with every call, as
 // kernel parameters (a graph captures them, nothing is uploaded), at most kMaxPointers a launch; longer lists take several launches.
 // No warp waits for another: block sums are written out and added up, in a fixed order, by whoever needs the norm next.
@@ -27,32 +27,38 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kBlocksPerSm = 4;
-constexpr int kItemBytes = 4096;
-constexpr int kUnroll = kItemBytes / (32 * 16);   // 16-byte loads per lane and item
 constexpr int kMaxPointers = 2000;                // two lists of 8-byte pointers within the 32,764 bytes of kernel parameters
+constexpr int64_t kMostElements = (int64_t)1 << 40; // a warp counts its lines and their elements in 32 bits
+constexpr int kMinLines = 8;                      // a warp's, before the list gets another one
+constexpr int kBatch = 8;                         // lines that a warp loads at once
+
+// Lines: 512 bytes of a tensor's own type (one 16-byte word a lane) where the tensor alone is walked, 128 elements (four a lane) where
+// it goes beside its part of a flat vector.
+enum { BY_BYTES = 0, BY_ELEMENTS = 1 };
 
 struct TensorInfo {
     int64_t numel;
     int64_t flat;          // offset in the flat vector
-    int64_t items;         // 4 KB items, wherever in a 16-byte word the tensor starts
+    int64_t lines[2];      // wherever between two boundaries the tensor starts
     int32_t type;
-    int32_t seg_first;     // partial sums of this tensor alone: one for each warp that has items of it
+    int32_t seg_first;     // partial sums of this tensor alone, one for each warp that has lines of it
     int32_t seg_count;
     int32_t pad;
 };
 
-struct WarpStart {         // where a warp's items begin; the next entry says where they end
-    int64_t item;          // within the tensor
-    int64_t index;         // within the launch
-    int32_t tensor;
-    int32_t pad;
+struct WarpWork {          // a warp's lines, and what it has to know of the tensor that it begins with: one fetch
+    int64_t at;            // upwards: the first line; downwards: behind the last one
+    int64_t numel, flat, lines;
+    int32_t left, tensor, type, pad;
 };
+
+enum { UP_BYTES = 0, DOWN_BYTES = 1, DOWN_ELEMENTS = 2 };
 
 struct Part {              // the tensors of one launch
     int first, count;
-    int blocks;
     int block0;            // of the partial sums
-    int64_t starts;        // into the table of WarpStart
+    int blocks[3];
+    int64_t works[3];      // into the table of WarpWork
 };
 
 template <int N>
@@ -86,9 +92,34 @@ struct Elements<DRACO_F16> {
     static __device__ __half round(float x) { return __float2half_rn(x); }
 };
 
+// N neighbouring elements as they lie in memory.
 template <int TYPE, int N>
 struct alignas(N * size_of(TYPE)) Vec {
-    typename Elements<TYPE>::type e[N];
+    uint32_t w[N * size_of(TYPE) / 4];
+    __device__ typename Elements<TYPE>::type element(int i) const {
+        typename Elements<TYPE>::type x;
+        if (TYPE == DRACO_F32) {
+            memcpy(&x, &w[i], sizeof(x));
+        } else {
+            const uint16_t half = (uint16_t)(w[i / 2] >> (i & 1) * 16);
+            memcpy(&x, &half, sizeof(x));
+        }
+        return x;
+    }
+    __device__ float value(int i) const { return Elements<TYPE>::value(element(i)); }
+    __device__ void set(const float (&x)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4 / size_of(TYPE)) {
+            if (TYPE == DRACO_F32) w[i] = __float_as_uint(x[i]);
+            else if (TYPE == DRACO_BF16) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(x[i], x[i + 1]);
+                memcpy(&w[i / 2], &h, 4);
+            } else {
+                const __half2 h = __floats2half2_rn(x[i], x[i + 1]);
+                memcpy(&w[i / 2], &h, 4);
+            }
+        }
+    }
 };
 
 // ---- sums of squares and largest magnitudes, in 64-bit slots ----
@@ -109,26 +140,26 @@ struct SumSquares {
     static __device__ void word(Slot& a, const Vec<TYPE, N>& v) {
         if (TYPE == DRACO_F32) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) one<TYPE>(a, v.e[i]);
+            for (int i = 0; i < N; ++i) one<TYPE>(a, v.element(i));
         } else {
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float x = Elements<TYPE>::value(v.e[i]);
+                const float x = v.value(i);
                 s = fmaf(x, x, s);
             }
             if (TYPE == DRACO_F16 || (s >= 0x1p-100f && s <= 0x1p120f)) {
                 a += (double)s;
             } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) one<TYPE>(a, v.e[i]);
+                for (int i = 0; i < N; ++i) one<TYPE>(a, v.element(i));
             }
         }
     }
     static __device__ double norm(Slot a) { return sqrt(a); }
 };
 
-// Magnitudes compare like their bit patterns, infinity above all numbers and NaN above infinity.
+// Magnitudes compare like their bit patterns, infinity above all numbers and NaN above infinity; 16-bit ones two at a time.
 struct MaxMagnitude {
     typedef unsigned long long Slot;
     static __device__ Slot zero() { return 0; }
@@ -140,8 +171,18 @@ struct MaxMagnitude {
     }
     template <int TYPE, int N>
     static __device__ void word(Slot& a, const Vec<TYPE, N>& v) {
+        if (TYPE == DRACO_F32) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) one<TYPE>(a, v.e[i]);
+            for (int i = 0; i < N; ++i) one<TYPE>(a, v.element(i));
+        } else {
+            unsigned m = 0;
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) m = __vmaxu2(m, v.w[i] & 0x7fff7fffu);
+            const unsigned short largest = (unsigned short)max(m & 0xffffu, m >> 16);
+            typename Elements<TYPE>::type x;
+            memcpy(&x, &largest, sizeof(x));
+            one<TYPE>(a, x);
+        }
     }
     static __device__ double norm(Slot a) { return (double)__uint_as_float((unsigned)a); }
 };
@@ -204,73 +245,141 @@ __device__ Factor block_factor(const Limit& l) {
     return factor_of(n, l.max_norm);
 }
 
-// ---- the walk over a warp's items ----
+// ---- the walk over a warp's lines ----
 
-// f(tensor, info, first item, items) for every tensor that the warp has items of.
-template <class F>
-__device__ void walk(const TensorInfo* __restrict__ infos, const WarpStart* __restrict__ starts, F f) {
-    const int w = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const WarpStart s = starts[w];
-    int64_t left = starts[w + 1].index - s.index, item = s.item;
-    for (int t = s.tensor; left > 0; ++t, item = 0) {
-        const TensorInfo& info = infos[t];
-        const int64_t take = min(left, info.items - item);
-        if (take > 0) f(t, info, item, take);
-        left -= max(take, (int64_t)0);
+// f(index, type, offset in the flat vector, numel, first line, lines) for every tensor that the warp has lines of, along the list or (DOWN)
+// back: a second pass over the list begins where the first one ended, with what is still in L2.  Tables do not change: the first of
+// them is read before the kernel waits for its predecessors.
+template <bool DOWN, int BY>
+struct Walk {
+    const WarpWork k;
+    const TensorInfo* const infos;
+    __device__ Walk(const TensorInfo* infos_, const WarpWork* __restrict__ works) : k(works[blockIdx.x * kWarps + (threadIdx.x >> 5)]), infos(infos_) {}
+    template <class F>
+    __device__ __forceinline__ void operator()(F f) const {
+        int left = k.left, t = k.tensor, type = k.type;
+        int64_t at = k.at, numel = k.numel, flat = k.flat, lines = k.lines;
+        while (left > 0) {
+            const int take = (int)min((int64_t)left, DOWN ? at : lines - at);
+            if (take > 0) f(t, type, flat, numel, DOWN ? at - take : at, take);
+            left -= take;
+            if (left <= 0) break;
+            t += DOWN ? -1 : 1;
+            const TensorInfo* i = infos + t;
+            numel = i->numel;
+            flat = i->flat;
+            lines = i->lines[BY];
+            type = i->type;
+            at = DOWN ? lines : 0;
+        }
     }
-}
+};
 
 template <class F>
-__device__ void by_type(int type, F f) {
+__device__ __forceinline__ void by_type(int type, F f) {
     if (type == DRACO_F32) f(std::integral_constant<int, DRACO_F32>());
     else if (type == DRACO_BF16) f(std::integral_constant<int, DRACO_BF16>());
     else f(std::integral_constant<int, DRACO_F16>());
 }
 
-template <class K, int TYPE>
-__device__ void measure_items(const void* base, int64_t numel, int64_t item, int64_t take, typename K::Slot& acc) {
-    constexpr int kVec = 16 / size_of(TYPE), kItem = kItemBytes / size_of(TYPE);
-    typedef typename Elements<TYPE>::type T;
-    const int lane = threadIdx.x & 31;
-    const int shift = (int)((reinterpret_cast<uintptr_t>(base) & 15u) / size_of(TYPE));
-    const T* p = static_cast<const T*>(base);
-    for (int64_t lo = item * kItem - shift; take > 0; --take, lo += kItem) {
-        if (lo >= 0 && lo + kItem <= numel) {
-            const Vec<TYPE, kVec>* v = reinterpret_cast<const Vec<TYPE, kVec>*>(p + lo) + lane;
-            Vec<TYPE, kVec> x[kUnroll];
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) x[u] = v[u * 32];
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) K::template word<TYPE, kVec>(acc, x[u]);
-        } else {
-            for (int u = 0; u < kUnroll; ++u) {
-                const int64_t e = lo + (u * 32 + lane) * kVec;
-                if (e >= 0 && e + kVec <= numel) {
-                    K::template word<TYPE, kVec>(acc, *reinterpret_cast<const Vec<TYPE, kVec>*>(p + e));
-                } else {
-                    for (int i = 0; i < kVec; ++i)
-                        if (e + i >= 0 && e + i < numel) K::template one<TYPE>(acc, p[e + i]);
-                }
-            }
+template <class F>
+__device__ __forceinline__ void by_alignment(bool aligned, F f) {
+    if (aligned) f(std::true_type());
+    else f(std::false_type());
+}
+
+// A warp's part of a tensor: lines of VEC elements a lane, the first of which begins `origin` elements into the tensor (negative at its start,
+// where the tensor begins behind a word's boundary).  Elements origin + begin .. origin + end - 1 are the tensor's.
+template <int VEC>
+struct Range {
+    int64_t origin;
+    int take, begin, end;
+    __device__ Range(int64_t numel, int shift, int64_t line, int take_)
+        : origin(line * 32 * VEC - shift), take(take_), begin(origin < 0 ? shift : 0), end((int)max(min(numel - origin, (int64_t)take_ * 32 * VEC), (int64_t)0)) {}   // the last line may lie behind the tensor
+
+    // batch(at, low, high) for BATCH lines at a time, `at` this lane's place (from origin on) in the first of them: its words u = 0 .. BATCH - 1,
+    // at + 32 VEC u, are all the tensor's where low <= u * 32 VEC <= high.
+    template <bool DOWN, int BATCH, class F>
+    __device__ __forceinline__ void batches(F batch) const {
+        const int lane = (threadIdx.x & 31) * VEC, count = (take + BATCH - 1) / BATCH;
+        for (int i = 0; i < count; ++i) {
+            const int at = (DOWN ? count - 1 - i : i) * (BATCH * 32 * VEC) + lane;
+            batch(at, begin - at, end - VEC - at);
         }
     }
+
+    // single(i) for the elements of a word that reaches over one of the tensor's ends, a lane each.
+    template <class F>
+    __device__ __forceinline__ void ends(F single) const {
+        const int lane = threadIdx.x & 31, tail = end & ~(VEC - 1);
+        if (begin > 0 && lane >= begin && lane < min(VEC, end)) single(lane);
+        if (tail + lane < end && (tail > 0 || begin == 0)) single(tail + lane);
+    }
+};
+
+#define DRACO_WHOLE(u) ((u) * 32 * kVec >= low && (u) * 32 * kVec <= high)
+
+template <int TYPE>
+__device__ int behind_word(const void* p) { return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / size_of(TYPE)); }
+
+// Zeros where `here` is false.
+template <int TYPE, int N, bool ALIGNED>
+__device__ __forceinline__ Vec<TYPE, N> load(bool here, const typename Elements<TYPE>::type* p) {
+    Vec<TYPE, N> v = {};
+    if (!here) return v;
+    if (ALIGNED) return *reinterpret_cast<const Vec<TYPE, N>*>(p);
+    if (TYPE == DRACO_F32) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) v.w[i / 2] = reinterpret_cast<const uint16_t*>(p)[i] | (uint32_t)reinterpret_cast<const uint16_t*>(p)[i + 1] << 16;
+    }
+    return v;
+}
+
+template <int TYPE, int N, bool ALIGNED>
+__device__ __forceinline__ void store(typename Elements<TYPE>::type* p, const Vec<TYPE, N>& v) {
+    if (ALIGNED) {
+        *reinterpret_cast<Vec<TYPE, N>*>(p) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = v.element(i);
+    }
+}
+
+template <class K, int TYPE>
+__device__ __forceinline__ void measure_lines(const void* base, int64_t numel, int64_t line, int take, typename K::Slot& acc) {
+    constexpr int kVec = 16 / size_of(TYPE);
+    typedef typename Elements<TYPE>::type T;
+    typedef Vec<TYPE, kVec> V;
+    const Range<kVec> range(numel, behind_word<TYPE>(base), line, take);
+    const T* p = static_cast<const T*>(base) + range.origin;
+    range.template batches<false, kBatch>([&](int at, int low, int high) {
+        V x[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) x[u] = load<TYPE, kVec, true>(DRACO_WHOLE(u), p + at + u * 32 * kVec);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) K::template word<TYPE, kVec>(acc, x[u]);
+    });
+    range.ends([&](int i) { K::template one<TYPE>(acc, p[i]); });
 }
 
 // Block sums to slots[blockIdx.x]; SEGMENTS: the sums of each warp's part of each tensor to segments[warp + tensor], a place of its
 // own for every such pair since both only ever grow along the list.  norm: written by the block that finishes last.
 template <class K, int N, bool SEGMENTS>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
-measure_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const WarpStart* __restrict__ starts,
+measure_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const WarpWork* __restrict__ works,
                typename K::Slot* slots, int block0, typename K::Slot* segments, float* norm, int all_blocks, unsigned* ticket) {
+    const Walk<false, BY_BYTES> walk(infos, works);
     pdl_begin();
     __shared__ typename K::Slot shared[kWarps];
     __shared__ bool last;
     typename K::Slot acc = K::zero();
     const int w = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    walk(infos, starts, [&](int t, const TensorInfo& info, int64_t item, int64_t take) {
+    walk([&](int t, int type_, int64_t, int64_t numel, int64_t line, int take) {
         typename K::Slot a = K::zero();
-        if (list.p[t])
-            by_type(info.type, [&](auto type) { measure_items<K, decltype(type)::value>(list.p[t], info.numel, item, take, SEGMENTS ? a : acc); });
+        if (list.p[t]) by_type(type_, [&](auto type) { measure_lines<K, decltype(type)::value>(list.p[t], numel, line, take, SEGMENTS ? a : acc); });
         if (SEGMENTS) {
             a = warp_total<K>(a);
             if ((threadIdx.x & 31) == 0) {
@@ -317,182 +426,176 @@ each_kernel(const TensorInfo* __restrict__ infos, int count, const typename K::S
     }
 }
 
+// The words of what is written; an input that lies otherwise is read element by element, from L1 but for the first of each word.
 template <int TYPE>
-__device__ typename Elements<TYPE>::type scaled(typename Elements<TYPE>::type x, float c) {
-    return Elements<TYPE>::round(Elements<TYPE>::value(x) * c);
-}
-
-template <int TYPE>
-__device__ void scale_items(const void* from, void* to, int64_t numel, int64_t item, int64_t take, float c) {
-    constexpr int kVec = 16 / size_of(TYPE), kItem = kItemBytes / size_of(TYPE);
+__device__ __forceinline__ void scale_lines(const void* from, void* to, int64_t numel, int64_t line, int take, float c) {
+    constexpr int kVec = 16 / size_of(TYPE);
     typedef typename Elements<TYPE>::type T;
-    const int lane = threadIdx.x & 31;
-    const int shift = (int)((reinterpret_cast<uintptr_t>(from) & 15u) / size_of(TYPE));
-    const bool together = ((reinterpret_cast<uintptr_t>(from) ^ reinterpret_cast<uintptr_t>(to)) & 15u) == 0;
-    const T* p = static_cast<const T*>(from);
-    T* q = static_cast<T*>(to);
-    for (int64_t lo = item * kItem - shift; take > 0; --take, lo += kItem) {
-        if (together && lo >= 0 && lo + kItem <= numel) {
-            const Vec<TYPE, kVec>* v = reinterpret_cast<const Vec<TYPE, kVec>*>(p + lo) + lane;
-            Vec<TYPE, kVec>* o = reinterpret_cast<Vec<TYPE, kVec>*>(q + lo) + lane;
-            Vec<TYPE, kVec> x[kUnroll];
+    typedef Vec<TYPE, kVec> V;
+    const int shift = behind_word<TYPE>(to);
+    const Range<kVec> range(numel, shift, line, take);
+    const T* p = static_cast<const T*>(from) + range.origin;
+    T* q = static_cast<T*>(to) + range.origin;
+    by_alignment(shift == behind_word<TYPE>(from), [&](auto how) {
+        constexpr bool ALIGNED = decltype(how)::value;
+        constexpr int kOnce = ALIGNED ? kBatch : 1;
+        range.template batches<true, kOnce>([&](int at, int low, int high) {
+            V x[kOnce];
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) x[u] = v[u * 32];
+            for (int u = 0; u < kOnce; ++u)
+                x[u] = load<TYPE, kVec, ALIGNED>(DRACO_WHOLE(u), p + at + u * 32 * kVec);
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
+            for (int u = 0; u < kOnce; ++u) {
+                float y[kVec];
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) x[u].e[i] = scaled<TYPE>(x[u].e[i], c);
-                o[u * 32] = x[u];
+                for (int i = 0; i < kVec; ++i) y[i] = x[u].value(i) * c;
+                x[u].set(y);
+                if (DRACO_WHOLE(u)) store<TYPE, kVec, true>(q + at + u * 32 * kVec, x[u]);
             }
-        } else {
-            for (int64_t e = max(lo, (int64_t)0) + lane; e < min(lo + kItem, numel); e += 32) q[e] = scaled<TYPE>(p[e], c);
-        }
-    }
+        });
+    });
+    range.ends([&](int i) { q[i] = Elements<TYPE>::round(Elements<TYPE>::value(p[i]) * c); });
 }
 
 // to = from * c.  In place nothing is written where c is 1.
 template <int N>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
 scale_kernel(const __grid_constant__ Pointers<N> from, const __grid_constant__ Pointers<N> to, const TensorInfo* __restrict__ infos,
-             const WarpStart* __restrict__ starts, Limit limit, const float* factors) {
+             const WarpWork* __restrict__ works, Limit limit, const float* factors) {
+    const Walk<true, BY_BYTES> walk(infos, works);
     pdl_begin();
     const float all = factors ? 1.0f : block_factor(limit).c;
-    walk(infos, starts, [&](int t, const TensorInfo& info, int64_t item, int64_t take) {
+    walk([&](int t, int type_, int64_t, int64_t numel, int64_t line, int take) {
         const float c = factors ? factors[t] : all;
         if (!from.p[t] || (c == 1.0f && from.p[t] == to.p[t])) return;
-        by_type(info.type, [&](auto type) { scale_items<decltype(type)::value>(from.p[t], to.p[t], info.numel, item, take, c); });
+        by_type(type_, [&](auto type) { scale_lines<decltype(type)::value>(from.p[t], to.p[t], numel, line, take, c); });
     });
 }
 
 // ---- a tensor beside its part of a flat fp32 vector: four elements a lane ----
 
+// Whether groups of four that begin `shift` elements before p are aligned.
 template <int TYPE>
-__device__ float4 load4(const typename Elements<TYPE>::type* p, bool aligned) {
-    Vec<TYPE, 4> v;
-    if (aligned) {
-        v = *reinterpret_cast<const Vec<TYPE, 4>*>(p);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v.e[i] = p[i];
-    }
-    return make_float4(Elements<TYPE>::value(v.e[0]), Elements<TYPE>::value(v.e[1]), Elements<TYPE>::value(v.e[2]), Elements<TYPE>::value(v.e[3]));
-}
-
-template <int TYPE>
-__device__ void store4(typename Elements<TYPE>::type* p, float4 x, bool aligned) {
-    Vec<TYPE, 4> v;
-    v.e[0] = Elements<TYPE>::round(x.x);
-    v.e[1] = Elements<TYPE>::round(x.y);
-    v.e[2] = Elements<TYPE>::round(x.z);
-    v.e[3] = Elements<TYPE>::round(x.w);
-    if (aligned) {
-        *reinterpret_cast<Vec<TYPE, 4>*>(p) = v;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = v.e[i];
-    }
-}
-
-// whole(e): elements e .. e + 3; single(e): one element, at the tensor's ends.  Items start `shift` elements early.
-template <int TYPE, class W, class S>
-__device__ void by_fours(int shift, int64_t numel, int64_t item, int64_t take, W whole, S single) {
-    constexpr int kItem = kItemBytes / size_of(TYPE);
-    const int lane = threadIdx.x & 31;
-    for (int64_t lo = item * kItem - shift; take > 0; --take, lo += kItem) {
-#pragma unroll 4
-        for (int u = 0; u < kItem / 128; ++u) {
-            const int64_t e = lo + u * 128 + lane * 4;
-            if (e >= 0 && e + 4 <= numel) {
-                whole(e);
-            } else {
-                for (int i = 0; i < 4; ++i)
-                    if (e + i >= 0 && e + i < numel) single(e + i);
-            }
-        }
-    }
-}
-
-template <int TYPE>
-__device__ bool fours_at(const typename Elements<TYPE>::type* p, int shift) {
+__device__ bool fours_at(const void* p, int shift) {
     return ((reinterpret_cast<uintptr_t>(p) - (uintptr_t)shift * size_of(TYPE)) & (4 * size_of(TYPE) - 1)) == 0;
+}
+
+// The groups of four are the row's.
+template <int TYPE>
+__device__ __forceinline__ void pack_lines(const void* base, float* out, int64_t numel, int64_t line, int take, float c) {
+    constexpr int kVec = 4;
+    typedef typename Elements<TYPE>::type T;
+    const int shift = (int)((reinterpret_cast<uintptr_t>(out) >> 2) & 3);
+    const Range<kVec> range(numel, shift, line, take);
+    const T* p = static_cast<const T*>(base) + range.origin;
+    float* q = out + range.origin;
+    by_alignment(fours_at<TYPE>(base, shift), [&](auto how) {
+        constexpr bool ALIGNED = decltype(how)::value;
+        constexpr int kOnce = ALIGNED ? kBatch : 2;
+        range.template batches<true, kOnce>([&](int at, int low, int high) {
+            Vec<TYPE, kVec> x[kOnce];
+#pragma unroll
+            for (int u = 0; u < kOnce; ++u)
+                x[u] = load<TYPE, kVec, ALIGNED>(DRACO_WHOLE(u), p + at + u * 32 * kVec);
+#pragma unroll
+            for (int u = 0; u < kOnce; ++u)
+                if (DRACO_WHOLE(u))
+                    *reinterpret_cast<float4*>(q + at + u * 32 * kVec) = make_float4(x[u].value(0) * c, x[u].value(1) * c, x[u].value(2) * c, x[u].value(3) * c);
+        });
+    });
+    range.ends([&](int i) { q[i] = Elements<TYPE>::value(p[i]) * c; });
 }
 
 // row[flat + i] = c * tensor[i]; zeros for a tensor that is absent.
 template <int N>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
-pack_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const WarpStart* __restrict__ starts, float* row, Limit limit) {
+pack_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const WarpWork* __restrict__ works, float* row, Limit limit) {
+    const Walk<true, BY_ELEMENTS> walk(infos, works);
     pdl_begin();
     const float c = block_factor(limit).c;
-    walk(infos, starts, [&](int t, const TensorInfo& info, int64_t item, int64_t take) {
-        float* out = row + info.flat;
-        const int shift = (int)((reinterpret_cast<uintptr_t>(out) >> 2) & 3);
-        by_type(info.type, [&](auto type) {
-            constexpr int TYPE = decltype(type)::value;
-            typedef typename Elements<TYPE>::type T;
-            const T* p = static_cast<const T*>(list.p[t]);
-            if (!p) {
-                by_fours<TYPE>(shift, info.numel, item, take, [&](int64_t e) { store4<DRACO_F32>(out + e, make_float4(0.f, 0.f, 0.f, 0.f), true); },
-                               [&](int64_t e) { out[e] = 0.0f; });
-                return;
-            }
-            const bool aligned = fours_at<TYPE>(p, shift);
-            by_fours<TYPE>(shift, info.numel, item, take,
-                           [&](int64_t e) {
-                               const float4 x = load4<TYPE>(p + e, aligned);
-                               store4<DRACO_F32>(out + e, make_float4(x.x * c, x.y * c, x.z * c, x.w * c), true);
-                           },
-                           [&](int64_t e) { out[e] = Elements<TYPE>::value(p[e]) * c; });
+    walk([&](int t, int type_, int64_t flat, int64_t numel, int64_t line, int take) {
+        if (list.p[t]) {
+            by_type(type_, [&](auto type) { pack_lines<decltype(type)::value>(list.p[t], row + flat, numel, line, take, c); });
+            return;
+        }
+        constexpr int kVec = 4;
+        const Range<kVec> range(numel, (int)((reinterpret_cast<uintptr_t>(row + flat) >> 2) & 3), line, take);
+        float* q = row + flat + range.origin;
+        range.template batches<true, kBatch>([&](int at, int low, int high) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+                if (DRACO_WHOLE(u)) *reinterpret_cast<float4*>(q + at + u * 32 * kVec) = make_float4(0.f, 0.f, 0.f, 0.f);
         });
+        range.ends([&](int i) { q[i] = 0.0f; });
     });
 }
 
-__device__ float4 step4(float4 w, float4 u, float s) {
-    return make_float4(fmaf(-s, u.x, w.x), fmaf(-s, u.y, w.y), fmaf(-s, u.z, w.z), fmaf(-s, u.w, w.w));
+// The groups of four are those of the side that is both read and written: w, or the master copy of it.
+template <int TYPE, bool MASTER>
+__device__ __forceinline__ void update_lines(void* base, const float* u, float* master, int64_t flat, int64_t numel, int64_t line, int take, float s) {
+    constexpr int kVec = 4, OLD = MASTER ? DRACO_F32 : TYPE;
+    typedef typename Elements<TYPE>::type T;
+    typedef typename Elements<OLD>::type O;
+    const int shift = MASTER ? (int)(flat & 3) : (int)((reinterpret_cast<uintptr_t>(base) / size_of(TYPE)) & 3);
+    const Range<kVec> range(numel, shift, line, take);
+    T* w = static_cast<T*>(base) + range.origin;
+    const float* from = u + flat + range.origin;
+    O* o = MASTER ? reinterpret_cast<O*>(master + flat + range.origin) : reinterpret_cast<O*>(w);
+    by_alignment(MASTER ? fours_at<TYPE>(base, shift) : ((flat - shift) & 3) == 0, [&](auto how) {
+        constexpr bool ALIGNED = decltype(how)::value;     // the other side: u, or w beside its master copy
+        constexpr int kOnce = ALIGNED ? kBatch / 2 : 1;    // two inputs
+        range.template batches<true, kOnce>([&](int at, int low, int high) {
+            Vec<DRACO_F32, kVec> x[kOnce];
+            Vec<OLD, kVec> old[kOnce];
+#pragma unroll
+            for (int k = 0; k < kOnce; ++k) {
+                x[k] = load<DRACO_F32, kVec, MASTER || ALIGNED>(DRACO_WHOLE(k), from + at + k * 32 * kVec);
+                old[k] = load<OLD, kVec, true>(DRACO_WHOLE(k), o + at + k * 32 * kVec);
+            }
+#pragma unroll
+            for (int k = 0; k < kOnce; ++k) {
+                float now[kVec];
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) now[i] = fmaf(-s, x[k].value(i), old[k].value(i));
+                Vec<TYPE, kVec> y;
+                y.set(now);
+                if (DRACO_WHOLE(k)) {
+                    if (MASTER) *reinterpret_cast<float4*>(o + at + k * 32 * kVec) = make_float4(now[0], now[1], now[2], now[3]);
+                    store<TYPE, kVec, !MASTER || ALIGNED>(w + at + k * 32 * kVec, y);
+                }
+            }
+        });
+    });
+    range.ends([&](int i) {
+        const float now = fmaf(-s, from[i], Elements<OLD>::value(o[i]));
+        if (MASTER) reinterpret_cast<float*>(o)[i] = now;
+        w[i] = Elements<TYPE>::round(now);
+    });
 }
 
 // w <- w - scale c u; MASTER: the fp32 master copy instead, and w is that, rounded.  Nothing where |u| is not finite.
 template <int N, bool MASTER>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
-update_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const WarpStart* __restrict__ starts,
+update_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const WarpWork* __restrict__ works,
               const float* __restrict__ u, float* __restrict__ master, float scale, Limit limit) {
+    const Walk<true, BY_ELEMENTS> walk(infos, works);
     pdl_begin();
     const Factor f = block_factor(limit);
     if (!f.finite) return;
     const float s = scale * f.c;
-    walk(infos, starts, [&](int t, const TensorInfo& info, int64_t item, int64_t take) {
-        if (!list.p[t]) return;
-        const float* from = u + info.flat;
-        float* m = MASTER ? master + info.flat : nullptr;
-        by_type(info.type, [&](auto type) {
-            constexpr int TYPE = decltype(type)::value;
-            typedef typename Elements<TYPE>::type T;
-            T* w = static_cast<T*>(list.p[t]);
-            // the grid of the side that is both read and written
-            const int shift = MASTER ? (int)(info.flat & 3) : (int)((reinterpret_cast<uintptr_t>(w) / size_of(TYPE)) & 3);
-            const bool flat_aligned = fours_at<DRACO_F32>(from, shift), w_aligned = fours_at<TYPE>(w, shift);
-            by_fours<TYPE>(shift, info.numel, item, take,
-                           [&](int64_t e) {
-                               const float4 x = load4<DRACO_F32>(from + e, flat_aligned);
-                               const float4 old = MASTER ? load4<DRACO_F32>(m + e, true) : load4<TYPE>(w + e, true);
-                               const float4 now = step4(old, x, s);
-                               if (MASTER) store4<DRACO_F32>(m + e, now, true);
-                               store4<TYPE>(w + e, now, w_aligned);
-                           },
-                           [&](int64_t e) {
-                               const float now = fmaf(-s, from[e], MASTER ? m[e] : Elements<TYPE>::value(w[e]));
-                               if (MASTER) m[e] = now;
-                               w[e] = Elements<TYPE>::round(now);
-                           });
-        });
+    walk([&](int t, int type_, int64_t flat, int64_t numel, int64_t line, int take) {
+        if (list.p[t]) by_type(type_, [&](auto type) { update_lines<decltype(type)::value, MASTER>(list.p[t], u, master, flat, numel, line, take, s); });
     });
 }
+
+#undef DRACO_WHOLE
 
 }  // namespace
 }  // namespace draco
 
 using namespace draco;
 
-// The sizes and types of a list, the split of its items over warps, and scratch for the partial sums.
+// The sizes and types of a list, the split of its lines over warps, and scratch for the partial sums.
 struct draco_layout {
     int count, device;
     int64_t size;
@@ -502,7 +605,7 @@ struct draco_layout {
     int num_parts;
     int all_blocks;
     TensorInfo* infos_dev;      // [count], then the flat vector's
-    WarpStart* starts_dev;
+    WarpWork* works_dev;
     void* slots_dev;            // [all_blocks], then [blocks of the flat vector]; 8 bytes each
     void* segments_dev;         // [warps + count]
     float* factors_dev;         // [count]
@@ -517,7 +620,7 @@ void free_layout(draco_layout* l) {
     free(l->type);
     free(l->parts);
     if (l->infos_dev) cudaFree(l->infos_dev);
-    if (l->starts_dev) cudaFree(l->starts_dev);
+    if (l->works_dev) cudaFree(l->works_dev);
     if (l->slots_dev) cudaFree(l->slots_dev);
     if (l->segments_dev) cudaFree(l->segments_dev);
     if (l->factors_dev) cudaFree(l->factors_dev);
@@ -525,42 +628,40 @@ void free_layout(draco_layout* l) {
     delete l;
 }
 
-int64_t items_of(int64_t numel, int type) {
-    const int64_t item = kItemBytes / size_of(type), early = 16 / size_of(type) - 1;
-    return numel ? (numel + early + item - 1) / item : 0;
+int64_t lines_of(int64_t numel, int per_lane) {            // the first line begins up to per_lane - 1 elements early
+    return numel ? (numel + per_lane - 1 + 32 * per_lane - 1) / (32 * per_lane) : 0;
 }
 
-// The WarpStarts of a part's tensors (infos[first ..]) and the tensors' segments; returns the number of blocks.
-int split(TensorInfo* infos, int first, int count, int sm_count, int seg0, WarpStart* starts) {
-    int64_t items = 0;
-    for (int t = first; t < first + count; ++t) items += infos[t].items;
-    const int64_t wanted = (items + kWarps - 1) / kWarps;
-    const int blocks = (int)(wanted < 1 ? 1 : wanted < (int64_t)sm_count * kBlocksPerSm ? wanted : (int64_t)sm_count * kBlocksPerSm);
+// The lines of infos[0 .. count - 1], dealt to warps in contiguous ranges of equal length; returns the number of blocks.
+int deal(const TensorInfo* infos, int count, int by, bool down, int sm_count, WarpWork* works) {
+    int64_t lines = 0;
+    for (int t = 0; t < count; ++t) lines += infos[t].lines[by];
+    const int64_t most = (int64_t)sm_count * kBlocksPerSm, wanted = (lines + kWarps * kMinLines - 1) / (kWarps * kMinLines);
+    const int blocks = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
     const int warps = blocks * kWarps;
-    const int used = items < warps ? (int)items : warps;   // the others have none: a tensor's segments are all written
-    int t = first;
-    int64_t before = 0;                                    // items of the tensors before t
-    for (int w = 0; w <= warps; ++w) {
-        const int64_t index = w < used ? items / used * w + items % used * w / used : items;
-        while (t < first + count - 1 && index >= before + infos[t].items) before += infos[t++].items;
-        starts[w].tensor = t - first;
-        starts[w].item = index - before;
-        starts[w].index = index;
-        starts[w].pad = 0;
-    }
-    int w = 0;
-    before = 0;
-    for (t = first; t < first + count; ++t) {
-        if (!infos[t].items) continue;
-        while (starts[w + 1].index <= before) ++w;         // the warp of the tensor's first item
-        int v = w;
-        while (starts[v + 1].index < before + infos[t].items) ++v;
-        infos[t].seg_first = seg0 + w + (t - first);
-        infos[t].seg_count = v - w + 1;
-        before += infos[t].items;
-        w = v;
+    const int used = lines < warps ? (int)lines : warps;   // the others have none: every warp between two others has lines
+    auto edge = [&](int w) { return w < used ? lines / used * w + lines % used * w / used : lines; };
+    int t = 0;
+    int64_t before = 0;                                    // lines of the tensors before t
+    for (int w = 0; w < warps; ++w) {
+        const int64_t begin = edge(w), end = edge(w + 1), here = down && end > begin ? end - 1 : begin;
+        while (t < count - 1 && here >= before + infos[t].lines[by]) before += infos[t++].lines[by];
+        works[w] = {down ? end - before : begin - before, infos[t].numel, infos[t].flat, infos[t].lines[by], (int32_t)(end - begin), t, infos[t].type, 0};
     }
     return blocks;
+}
+
+// The segments of infos[0 .. count - 1] by the works of deal(.., down = false): that of warp w and tensor t is number w + t.
+void number_segments(TensorInfo* infos, int count, const WarpWork* works, int warps) {
+    for (int w = 0; w < warps; ++w) {
+        int64_t left = works[w].left, at = works[w].at;
+        for (int t = works[w].tensor; left > 0; ++t, at = 0) {
+            const int64_t take = left < infos[t].lines[BY_BYTES] - at ? left : infos[t].lines[BY_BYTES] - at;
+            if (take <= 0) continue;
+            if (!infos[t].seg_count++) infos[t].seg_first = w + t;
+            left -= take;
+        }
+    }
 }
 
 template <class F>
@@ -584,7 +685,7 @@ int measure(draco_layout* l, const void* const* list, const float* u, int kind, 
         const Part& part = l->parts[list ? k : l->num_parts];
         Part given = part;
         if (!list) given.first = 0;
-        const int all = list ? l->all_blocks : part.blocks, block0 = list ? part.block0 : 0;
+        const int all = list ? l->all_blocks : part.blocks[UP_BYTES], block0 = list ? part.block0 : 0;
         char* slots = static_cast<char*>(l->slots_dev) + (list ? 0 : (size_t)l->all_blocks * 8);
         char* segs = static_cast<char*>(l->segments_dev) + 8 * ((size_t)part.block0 * kWarps + part.first);
         const int rc = with_capacity(part.count, [&](auto n) -> int {
@@ -592,8 +693,8 @@ int measure(draco_layout* l, const void* const* list, const float* u, int kind, 
             const Pointers<N> p = pointers_of<N>(list ? list : flat, given);
             auto go = [&](auto kernel, auto* slot) {
                 typedef decltype(slot) S;
-                launch_dependent(kernel, dim3(part.blocks), dim3(kThreads), 0, st, p, (const TensorInfo*)l->infos_dev + part.first,
-                                 (const WarpStart*)l->starts_dev + part.starts, (S)slots, block0, (S)segs, norm, all, l->ticket_dev);
+                launch_dependent(kernel, dim3(part.blocks[UP_BYTES]), dim3(kThreads), 0, st, p, (const TensorInfo*)l->infos_dev + part.first,
+                                 (const WarpWork*)l->works_dev + part.works[UP_BYTES], (S)slots, block0, (S)segs, norm, all, l->ticket_dev);
             };
             if (kind == DRACO_NORM_2) {
                 if (segments) go(measure_kernel<SumSquares, N, true>, (double*)nullptr);
@@ -692,8 +793,9 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
     if (count > DRACO_MAX_TENSORS) return DRACO_ELIMIT;
     int64_t size = 0;
     for (int t = 0; t < count; ++t) {
-        if (numel[t] < 0 || numel[t] > ((int64_t)1 << 48) || size > ((int64_t)1 << 48)) return DRACO_EINVAL;
+        if (numel[t] < 0) return DRACO_EINVAL;
         if (type[t] != DRACO_F32 && type[t] != DRACO_BF16 && type[t] != DRACO_F16) return DRACO_EINVAL;
+        if (numel[t] > kMostElements - size) return DRACO_ELIMIT;
         size += numel[t];
     }
     draco_layout* l = new (std::nothrow) draco_layout();
@@ -706,38 +808,44 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
     cudaError_t err = cudaGetDevice(&l->device);
     if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, l->device);
     if (err != cudaSuccess) { free_layout(l); return cuda_fail(err, "cudaGetDevice"); }
-    const int64_t most_starts = (int64_t)(l->num_parts + 1) * (sm_count * kBlocksPerSm * kWarps + 1);
+    const int64_t most_works = (int64_t)(3 * l->num_parts + 1) * sm_count * kBlocksPerSm * kWarps;
     l->numel = static_cast<int64_t*>(malloc(sizeof(int64_t) * count));
     l->type = static_cast<uint8_t*>(malloc(count));
-    l->parts = static_cast<Part*>(malloc(sizeof(Part) * (l->num_parts + 1)));
+    l->parts = static_cast<Part*>(calloc(l->num_parts + 1, sizeof(Part)));
     TensorInfo* infos = static_cast<TensorInfo*>(calloc(count + 1, sizeof(TensorInfo)));
-    WarpStart* starts = static_cast<WarpStart*>(malloc(sizeof(WarpStart) * most_starts));
+    WarpWork* works = static_cast<WarpWork*>(malloc(sizeof(WarpWork) * most_works));
     int rc = DRACO_OK;
-    if (!l->numel || !l->type || !l->parts || !infos || !starts) rc = DRACO_ENOMEM;
-    int64_t num_starts = 0;
-    int flat_blocks = 0;
+    if (!l->numel || !l->type || !l->parts || !infos || !works) rc = DRACO_ENOMEM;
+    int64_t num_works = 0;
     if (rc == DRACO_OK) {
         int64_t flat = 0;
-        for (int t = 0; t < count; ++t) {
-            l->numel[t] = infos[t].numel = numel[t];
-            l->type[t] = (uint8_t)(infos[t].type = type[t]);
-            infos[t].flat = flat;
-            infos[t].items = items_of(numel[t], type[t]);
-            flat += numel[t];
+        for (int t = 0; t <= count; ++t) {                 // the last: the flat vector
+            TensorInfo& i = infos[t];
+            i.numel = t < count ? numel[t] : size;
+            i.type = t < count ? type[t] : DRACO_F32;
+            i.flat = t < count ? flat : 0;
+            i.lines[BY_BYTES] = lines_of(i.numel, 16 / size_of(i.type));
+            i.lines[BY_ELEMENTS] = lines_of(i.numel, 4);
+            if (t == count) break;
+            l->numel[t] = i.numel;
+            l->type[t] = (uint8_t)i.type;
+            flat += i.numel;
         }
-        infos[count].numel = size;
-        infos[count].type = DRACO_F32;
-        infos[count].items = items_of(size, DRACO_F32);
         for (int k = 0; k <= l->num_parts; ++k) {
             Part& p = l->parts[k];
-            p.first = k < l->num_parts ? k * kMaxPointers : count;
-            p.count = k < l->num_parts ? (count - p.first < kMaxPointers ? count - p.first : kMaxPointers) : 1;
-            p.starts = num_starts;
+            const bool list = k < l->num_parts;
+            p.first = list ? k * kMaxPointers : count;
+            p.count = list ? (count - p.first < kMaxPointers ? count - p.first : kMaxPointers) : 1;
             p.block0 = l->all_blocks;
-            p.blocks = split(infos, p.first, p.count, sm_count, l->all_blocks * kWarps + p.first, starts + num_starts);
-            num_starts += p.blocks * kWarps + 1;
-            if (k < l->num_parts) l->all_blocks += p.blocks;
-            else flat_blocks = p.blocks;
+            for (int way = UP_BYTES; way <= (list ? DOWN_ELEMENTS : UP_BYTES); ++way) {
+                p.works[way] = num_works;
+                p.blocks[way] = deal(infos + p.first, p.count, way == DOWN_ELEMENTS ? BY_ELEMENTS : BY_BYTES, way != UP_BYTES, sm_count, works + num_works);
+                num_works += p.blocks[way] * kWarps;
+            }
+            if (!list) break;
+            number_segments(infos + p.first, p.count, works + p.works[UP_BYTES], p.blocks[UP_BYTES] * kWarps);
+            for (int t = p.first; t < p.first + p.count; ++t) infos[t].seg_first += p.block0 * kWarps + p.first;
+            l->all_blocks += p.blocks[UP_BYTES];
         }
     }
 #define DRACO_TRY(call)                                                                          \
@@ -747,20 +855,20 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
             if (e__ != cudaSuccess) rc = cuda_fail(e__, #call);                                  \
         }                                                                                        \
     } while (0)
-    const size_t slots = (size_t)l->all_blocks + flat_blocks;
+    const size_t slots = rc == DRACO_OK ? (size_t)l->all_blocks + l->parts[l->num_parts].blocks[UP_BYTES] : 0;
     DRACO_TRY(cudaMalloc(&l->infos_dev, sizeof(TensorInfo) * (count + 1)));
-    DRACO_TRY(cudaMalloc(&l->starts_dev, sizeof(WarpStart) * num_starts));
+    DRACO_TRY(cudaMalloc(&l->works_dev, sizeof(WarpWork) * num_works));
     DRACO_TRY(cudaMalloc(&l->slots_dev, 8 * slots));
     DRACO_TRY(cudaMalloc(&l->segments_dev, 8 * (slots * kWarps + count + 1)));
     DRACO_TRY(cudaMalloc(&l->factors_dev, sizeof(float) * count));
     DRACO_TRY(cudaMalloc(&l->ticket_dev, sizeof(unsigned)));
     DRACO_TRY(cudaMemset(l->ticket_dev, 0, sizeof(unsigned)));
     DRACO_TRY(cudaMemcpy(l->infos_dev, infos, sizeof(TensorInfo) * (count + 1), cudaMemcpyHostToDevice));
-    DRACO_TRY(cudaMemcpy(l->starts_dev, starts, sizeof(WarpStart) * num_starts, cudaMemcpyHostToDevice));
+    DRACO_TRY(cudaMemcpy(l->works_dev, works, sizeof(WarpWork) * num_works, cudaMemcpyHostToDevice));
     DRACO_TRY(cudaStreamSynchronize(nullptr));
 #undef DRACO_TRY
     free(infos);
-    free(starts);
+    free(works);
     if (rc != DRACO_OK) { free_layout(l); return rc; }
     *out = l;
     return DRACO_OK;
@@ -800,8 +908,8 @@ int draco_clip(draco_layout* layout, const void* const* tensors, void* const* ou
         const Limit limit = {layout->slots_dev, layout->all_blocks, kind, max_norm, k == 0 ? norm : nullptr};
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
-            launch_dependent(scale_kernel<N>, dim3(part.blocks), dim3(kThreads), 0, st, pointers_of<N>(tensors, part), pointers_of<N>(to, part),
-                             (const TensorInfo*)layout->infos_dev + part.first, (const WarpStart*)layout->starts_dev + part.starts, limit,
+            launch_dependent(scale_kernel<N>, dim3(part.blocks[DOWN_BYTES]), dim3(kThreads), 0, st, pointers_of<N>(tensors, part), pointers_of<N>(to, part),
+                             (const TensorInfo*)layout->infos_dev + part.first, (const WarpWork*)layout->works_dev + part.works[DOWN_BYTES], limit,
                              separately ? (const float*)layout->factors_dev + part.first : nullptr);
             DRACO_CUDA(cudaGetLastError());
             return DRACO_OK;
@@ -822,8 +930,8 @@ int draco_pack(draco_layout* layout, const void* const* tensors, int kind, float
         const Limit limit = {wanted ? layout->slots_dev : nullptr, layout->all_blocks, kind, max_norm, k == 0 ? norm : nullptr};
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
-            launch_dependent(pack_kernel<N>, dim3(part.blocks), dim3(kThreads), 0, st, pointers_of<N>(tensors, part),
-                             (const TensorInfo*)layout->infos_dev + part.first, (const WarpStart*)layout->starts_dev + part.starts, row, limit);
+            launch_dependent(pack_kernel<N>, dim3(part.blocks[DOWN_ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(tensors, part),
+                             (const TensorInfo*)layout->infos_dev + part.first, (const WarpWork*)layout->works_dev + part.works[DOWN_ELEMENTS], row, limit);
             DRACO_CUDA(cudaGetLastError());
             return DRACO_OK;
         });
@@ -846,12 +954,12 @@ int draco_update(draco_layout* layout, void* const* params, const float* u, floa
     for (int k = 0; k < layout->num_parts && rc == DRACO_OK; ++k) {
         const Part& part = layout->parts[k];
         const Limit limit = {wanted ? static_cast<char*>(layout->slots_dev) + (size_t)layout->all_blocks * 8 : nullptr,
-                             layout->parts[layout->num_parts].blocks, kind, max_norm, k == 0 ? norm : nullptr};
+                             layout->parts[layout->num_parts].blocks[UP_BYTES], kind, max_norm, k == 0 ? norm : nullptr};
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
             auto go = [&](auto kernel) {
-                launch_dependent(kernel, dim3(part.blocks), dim3(kThreads), 0, st, pointers_of<N>(params, part),
-                                 (const TensorInfo*)layout->infos_dev + part.first, (const WarpStart*)layout->starts_dev + part.starts, u, master, scale, limit);
+                launch_dependent(kernel, dim3(part.blocks[DOWN_ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(params, part),
+                                 (const TensorInfo*)layout->infos_dev + part.first, (const WarpWork*)layout->works_dev + part.works[DOWN_ELEMENTS], u, master, scale, limit);
             };
             if (master) go(update_kernel<N, true>);
             else go(update_kernel<N, false>);
