@@ -381,7 +381,7 @@ class Layout:
         return _TYPES[str(t)]
 
     def close(self):
-        if getattr(self, "_h", None):
+        if getattr(self, "_h", None) and lib is not None:       # None while the interpreter ends
             lib.draco_layout_destroy(self._h)
             self._h = None
             self._address = None

@@ -30,6 +30,12 @@ constexpr int kBlocksPerSm = 4;
 constexpr int kMaxPointers = 2000;                // two lists of 8-byte pointers within the 32,764 bytes of kernel parameters
 constexpr int64_t kMostElements = (int64_t)1 << 40; // a warp counts its lines and their elements in 32 bits
 constexpr int kMinLines = 8;                      // a warp's, before the list gets another one
+// Second passes of long lists: several waves of blocks with short chunks.  SMs that are further from memory take longer over the same share, and
+// with one wave the last of them holds the others up (138 M bf16 packed: one wave 201 us, chunks of 24 lines 185, of 12 182, of 8 181; with a
+// master copy updated, 60.2 M 186, 176, 173, 171).  Below kWaveLines lines a warp one wave is level or faster.
+constexpr int kWaveLines = 32, kWavesLines = 8, kWaves = 64;
+// In place most calls have nothing to write, and blocks that only find that out cost 1.2 us a thousand: always one wave (1.0e9 bf16 below the limit
+// 296 us, chunks of 64 lines 306, of 8 346; above it 966, 925, 901).
 constexpr int kBatch = 8;                         // lines that a warp loads at once
 
 // Lines: 512 bytes of a tensor's own type (one 16-byte word a lane) where the tensor alone is walked, 128 elements (four a lane) where
@@ -46,19 +52,26 @@ struct TensorInfo {
     int32_t pad;
 };
 
-struct WarpWork {          // a warp's lines, and what it has to know of the tensor that it begins with: one fetch
-    int64_t at;            // upwards: the first line; downwards: behind the last one
-    int64_t numel, flat, lines;
+struct Chunk {             // `left` neighbouring lines: upwards from line `at` of tensor `tensor`, or downwards from the one before it
+    int64_t at;
+    int64_t numel, flat, lines;    // of that tensor: known as soon as the chunk is
     int32_t left, tensor, type, pad;
 };
 
-enum { UP_BYTES = 0, DOWN_BYTES = 1, DOWN_ELEMENTS = 2 };
+// A chunk a warp, all of equal length.  MEASURE: upwards, one wave of blocks, which leave few sums to add up.  The second passes go
+// back, from the end of the list (and of each chunk), whose part is still in L2.
+enum { MEASURE = 0, IN_PLACE = 1, BYTES = 2, ELEMENTS = 3, TABLES = 4 };
 
 struct Part {              // the tensors of one launch
     int first, count;
     int block0;            // of the partial sums
-    int blocks[3];
-    int64_t works[3];      // into the table of WarpWork
+    int blocks[TABLES];
+    int64_t table[TABLES]; // into the table of chunks
+};
+
+struct Result {            // of a measurement
+    float c;
+    int finite;
 };
 
 template <int N>
@@ -207,73 +220,60 @@ __device__ typename K::Slot block_total(typename K::Slot a, typename K::Slot* sh
     return a;
 }
 
-template <class K>
-__device__ typename K::Slot total_of(const void* slots, int64_t first, int64_t count, typename K::Slot* shared) {
-    const typename K::Slot* s = static_cast<const typename K::Slot*>(slots) + first;
-    typename K::Slot a = K::zero();
-    for (int64_t i = threadIdx.x; i < count; i += kThreads) K::add(a, s[i]);
-    return block_total<K>(a, shared);
-}
-
+// Where a kernel gets the factor from: formed already, or to be formed from the sums by every block for itself, which one wave of blocks
+// has sooner than the measurement's last block would have it; null both: none is wanted.
 struct Limit {
-    const void* slots;     // block sums, or null: no norm is wanted
-    int count;
-    int kind;
+    const Result* result;
+    const void* slots;
+    int count, kind;
     float max_norm;
-    float* norm;           // may be null
+    float* norm;           // written by the first block if it forms the norm; may be null
 };
 
-struct Factor {
-    float c;
-    bool finite;
-};
-
-__device__ Factor factor_of(double norm, float max_norm) {
-    Factor f;
-    f.finite = isfinite((float)norm);
-    f.c = f.finite && norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f;
-    return f;
+__device__ Result result_of(double norm, float max_norm) {
+    Result r;
+    r.finite = isfinite((float)norm);
+    r.c = r.finite && norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f;
+    return r;
 }
 
-// The block sums added up and the factor they give, in every thread; the first block writes the norm down.
-__device__ Factor block_factor(const Limit& l) {
-    __shared__ unsigned long long shared[kWarps];
-    if (!l.slots) return Factor{1.0f, true};
-    const double n = l.kind == DRACO_NORM_2 ? SumSquares::norm(total_of<SumSquares>(l.slots, 0, l.count, reinterpret_cast<double*>(shared)))
-                                            : MaxMagnitude::norm(total_of<MaxMagnitude>(l.slots, 0, l.count, shared));
+template <class K>
+__device__ double norm_of(const void* slots, int first, int count) {
+    __shared__ typename K::Slot shared[kWarps];
+    typename K::Slot a = K::zero();
+    for (int i = threadIdx.x; i < count; i += kThreads) K::add(a, __ldcg(static_cast<const typename K::Slot*>(slots) + first + i));
+    return K::norm(block_total<K>(a, shared));
+}
+
+__device__ __forceinline__ Result factor(const Limit& l) {
+    if (l.result) return *l.result;
+    if (!l.slots) return Result{1.0f, 1};
+    const double n = l.kind == DRACO_NORM_2 ? norm_of<SumSquares>(l.slots, 0, l.count) : norm_of<MaxMagnitude>(l.slots, 0, l.count);
     if (l.norm && blockIdx.x == 0 && threadIdx.x == 0) *l.norm = (float)n;
-    return factor_of(n, l.max_norm);
+    return result_of(n, l.max_norm);
 }
 
 // ---- the walk over a warp's lines ----
 
-// f(index, type, offset in the flat vector, numel, first line, lines) for every tensor that the warp has lines of, along the list or (DOWN)
-// back: a second pass over the list begins where the first one ended, with what is still in L2.  Tables do not change: the first of
-// them is read before the kernel waits for its predecessors.
-template <bool DOWN, int BY>
-struct Walk {
-    const WarpWork k;
-    const TensorInfo* const infos;
-    __device__ Walk(const TensorInfo* infos_, const WarpWork* __restrict__ works) : k(works[blockIdx.x * kWarps + (threadIdx.x >> 5)]), infos(infos_) {}
-    template <class F>
-    __device__ __forceinline__ void operator()(F f) const {
-        int left = k.left, t = k.tensor, type = k.type;
-        int64_t at = k.at, numel = k.numel, flat = k.flat, lines = k.lines;
-        while (left > 0) {
-            const int take = (int)min((int64_t)left, DOWN ? at : lines - at);
-            if (take > 0) f(t, type, flat, numel, DOWN ? at - take : at, take);
-            left -= take;
-            if (left <= 0) break;
-            t += DOWN ? -1 : 1;
-            const TensorInfo* i = infos + t;
-            numel = i->numel;
-            flat = i->flat;
-            lines = i->lines[BY];
-            type = i->type;
-            at = DOWN ? lines : 0;
-        }
+// f(index, type, offset in the flat vector, numel, first line, lines) for every tensor that a chunk has lines of.
+template <bool DOWN, int BY, class F>
+__device__ __forceinline__ void walk(const TensorInfo* infos, const Chunk& chunk, F f) {
+    int left = chunk.left, t = chunk.tensor, type = chunk.type;
+    int64_t at = chunk.at, numel = chunk.numel, flat = chunk.flat, lines = chunk.lines;
+    while (left > 0) {
+        const int take = (int)min((int64_t)left, DOWN ? at : lines - at);
+        if (take > 0) f(t, type, flat, numel, DOWN ? at - take : at, take);
+        left -= take;
+        if (left <= 0) break;
+        t += DOWN ? -1 : 1;
+        const TensorInfo* i = infos + t;
+        numel = i->numel;
+        flat = i->flat;
+        lines = i->lines[BY];
+        type = i->type;
+        at = DOWN ? lines : 0;
     }
-};
+}
 
 template <class F>
 __device__ __forceinline__ void by_type(int type, F f) {
@@ -288,7 +288,7 @@ __device__ __forceinline__ void by_alignment(bool aligned, F f) {
     else f(std::false_type());
 }
 
-// A warp's part of a tensor: lines of VEC elements a lane, the first of which begins `origin` elements into the tensor (negative at its start,
+// A part of a tensor: lines of VEC elements a lane, the first of which begins `origin` elements into the tensor (negative at its start,
 // where the tensor begins behind a word's boundary).  Elements origin + begin .. origin + end - 1 are the tensor's.
 template <int VEC>
 struct Range {
@@ -301,7 +301,8 @@ struct Range {
     // at + 32 VEC u, are all the tensor's where low <= u * 32 VEC <= high.
     template <bool DOWN, int BATCH, class F>
     __device__ __forceinline__ void batches(F batch) const {
-        const int lane = (threadIdx.x & 31) * VEC, count = (take + BATCH - 1) / BATCH;
+        const int lane = (threadIdx.x & 31) * VEC;
+        const int count = (take + BATCH - 1) / BATCH;
         for (int i = 0; i < count; ++i) {
             const int at = (DOWN ? count - 1 - i : i) * (BATCH * 32 * VEC) + lane;
             batch(at, begin - at, end - VEC - at);
@@ -365,19 +366,20 @@ __device__ __forceinline__ void measure_lines(const void* base, int64_t numel, i
     range.ends([&](int i) { K::template one<TYPE>(acc, p[i]); });
 }
 
-// Block sums to slots[blockIdx.x]; SEGMENTS: the sums of each warp's part of each tensor to segments[warp + tensor], a place of its
-// own for every such pair since both only ever grow along the list.  norm: written by the block that finishes last.
+// Block sums to slots[blockIdx.x]; finish: the norm of all, too, from the block that finishes last.  SEGMENTS: the sums of each warp's part of each
+// tensor to segments[warp + tensor], a place of its own for every such pair, since both only grow along the list.
 template <class K, int N, bool SEGMENTS>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
-measure_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const WarpWork* __restrict__ works,
-               typename K::Slot* slots, int block0, typename K::Slot* segments, float* norm, int all_blocks, unsigned* ticket) {
-    const Walk<false, BY_BYTES> walk(infos, works);
+measure_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks,
+               typename K::Slot* slots, int block0, int all_blocks, unsigned* ticket, typename K::Slot* segments, bool finish, float max_norm,
+               float* norm, Result* result) {
+    const int w = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const Chunk chunk = chunks[w];
     pdl_begin();
     __shared__ typename K::Slot shared[kWarps];
     __shared__ bool last;
     typename K::Slot acc = K::zero();
-    const int w = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    walk([&](int t, int type_, int64_t, int64_t numel, int64_t line, int take) {
+    walk<false, BY_BYTES>(infos, chunk, [&](int t, int type_, int64_t, int64_t numel, int64_t line, int take) {
         typename K::Slot a = K::zero();
         if (list.p[t]) by_type(type_, [&](auto type) { measure_lines<K, decltype(type)::value>(list.p[t], numel, line, take, SEGMENTS ? a : acc); });
         if (SEGMENTS) {
@@ -391,38 +393,37 @@ measure_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __res
     acc = block_total<K>(acc, shared);
     if (threadIdx.x == 0) {
         slots[block0 + blockIdx.x] = acc;
-        if (norm) {
+        if (finish) {
             __threadfence();
-            last = atomicInc(ticket, all_blocks - 1) == all_blocks - 1;     // back at zero after the last
+            last = atomicInc(ticket, all_blocks - 1) == all_blocks - 1; // back at zero after the last
             __threadfence();
         }
     }
-    if (!norm) return;
+    if (!finish) return;
     __syncthreads();
     if (!last) return;
-    typename K::Slot a = K::zero();
-    for (int i = threadIdx.x; i < all_blocks; i += kThreads) K::add(a, __ldcg(slots + i));
-    a = block_total<K>(a, shared);
-    if (threadIdx.x == 0) *norm = (float)K::norm(a);
+    const double n = norm_of<K>(slots, 0, all_blocks);
+    if (threadIdx.x == 0) {
+        if (norm) *norm = (float)n;
+        if (result) *result = result_of(n, max_norm);
+    }
 }
 
 // One block a tensor: its segments added up, its norm and factor; one block more: the norm of all.
 template <class K>
 __global__ void __launch_bounds__(kThreads)
-each_kernel(const TensorInfo* __restrict__ infos, int count, const typename K::Slot* segments, const typename K::Slot* slots, int all_blocks,
-            float max_norm, float* norm, float* each, float* factors) {
+each_kernel(const TensorInfo* __restrict__ infos, const typename K::Slot* segments, const typename K::Slot* slots, int all_blocks, float max_norm,
+            float* norm, float* each, float* factors) {
+    const bool all = blockIdx.x == gridDim.x - 1;
+    const int first = all ? 0 : infos[blockIdx.x].seg_first, count = all ? all_blocks : infos[blockIdx.x].seg_count;
     pdl_begin();
-    __shared__ typename K::Slot shared[kWarps];
-    if (blockIdx.x == count) {
-        const double n = K::norm(total_of<K>(slots, 0, all_blocks, shared));
-        if (norm && threadIdx.x == 0) *norm = (float)n;
-        return;
-    }
-    const TensorInfo& info = infos[blockIdx.x];
-    const double n = K::norm(total_of<K>(segments, info.seg_first, info.seg_count, shared));
-    if (threadIdx.x == 0) {
+    const double n = norm_of<K>(all ? slots : segments, first, count);
+    if (threadIdx.x != 0) return;
+    if (all) {
+        if (norm) *norm = (float)n;
+    } else {
         if (each) each[blockIdx.x] = (float)n;
-        if (factors) factors[blockIdx.x] = factor_of(n, max_norm).c;
+        if (factors) factors[blockIdx.x] = result_of(n, max_norm).c;
     }
 }
 
@@ -461,11 +462,12 @@ __device__ __forceinline__ void scale_lines(const void* from, void* to, int64_t 
 template <int N>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
 scale_kernel(const __grid_constant__ Pointers<N> from, const __grid_constant__ Pointers<N> to, const TensorInfo* __restrict__ infos,
-             const WarpWork* __restrict__ works, Limit limit, const float* factors) {
-    const Walk<true, BY_BYTES> walk(infos, works);
+             const Chunk* __restrict__ chunks, Limit limit, const float* factors, bool in_place) {
+    const Chunk chunk = chunks[(gridDim.x - 1 - blockIdx.x) * kWarps + (threadIdx.x >> 5)];
     pdl_begin();
-    const float all = factors ? 1.0f : block_factor(limit).c;
-    walk([&](int t, int type_, int64_t, int64_t numel, int64_t line, int take) {
+    const float all = factors ? 1.0f : factor(limit).c;
+    if (in_place && !factors && all == 1.0f) return;
+    walk<true, BY_BYTES>(infos, chunk, [&](int t, int type_, int64_t, int64_t numel, int64_t line, int take) {
         const float c = factors ? factors[t] : all;
         if (!from.p[t] || (c == 1.0f && from.p[t] == to.p[t])) return;
         by_type(type_, [&](auto type) { scale_lines<decltype(type)::value>(from.p[t], to.p[t], numel, line, take, c); });
@@ -509,11 +511,11 @@ __device__ __forceinline__ void pack_lines(const void* base, float* out, int64_t
 // row[flat + i] = c * tensor[i]; zeros for a tensor that is absent.
 template <int N>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
-pack_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const WarpWork* __restrict__ works, float* row, Limit limit) {
-    const Walk<true, BY_ELEMENTS> walk(infos, works);
+pack_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks, float* row, Limit limit) {
+    const Chunk chunk = chunks[(gridDim.x - 1 - blockIdx.x) * kWarps + (threadIdx.x >> 5)];
     pdl_begin();
-    const float c = block_factor(limit).c;
-    walk([&](int t, int type_, int64_t flat, int64_t numel, int64_t line, int take) {
+    const float c = factor(limit).c;
+    walk<true, BY_ELEMENTS>(infos, chunk, [&](int t, int type_, int64_t flat, int64_t numel, int64_t line, int take) {
         if (list.p[t]) {
             by_type(type_, [&](auto type) { pack_lines<decltype(type)::value>(list.p[t], row + flat, numel, line, take, c); });
             return;
@@ -576,14 +578,14 @@ __device__ __forceinline__ void update_lines(void* base, const float* u, float* 
 // w <- w - scale c u; MASTER: the fp32 master copy instead, and w is that, rounded.  Nothing where |u| is not finite.
 template <int N, bool MASTER>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
-update_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const WarpWork* __restrict__ works,
+update_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks,
               const float* __restrict__ u, float* __restrict__ master, float scale, Limit limit) {
-    const Walk<true, BY_ELEMENTS> walk(infos, works);
+    const Chunk chunk = chunks[(gridDim.x - 1 - blockIdx.x) * kWarps + (threadIdx.x >> 5)];
     pdl_begin();
-    const Factor f = block_factor(limit);
-    if (!f.finite) return;
-    const float s = scale * f.c;
-    walk([&](int t, int type_, int64_t flat, int64_t numel, int64_t line, int take) {
+    const Result r = factor(limit);
+    if (!r.finite) return;
+    const float s = scale * r.c;
+    walk<true, BY_ELEMENTS>(infos, chunk, [&](int t, int type_, int64_t flat, int64_t numel, int64_t line, int take) {
         if (list.p[t]) by_type(type_, [&](auto type) { update_lines<decltype(type)::value, MASTER>(list.p[t], u, master, flat, numel, line, take, s); });
     });
 }
@@ -604,11 +606,13 @@ struct draco_layout {
     Part* parts;                // [num_parts], then that of the flat vector
     int num_parts;
     int all_blocks;
+    int sm_count;
     TensorInfo* infos_dev;      // [count], then the flat vector's
-    WarpWork* works_dev;
+    Chunk* chunks_dev;
     void* slots_dev;            // [all_blocks], then [blocks of the flat vector]; 8 bytes each
     void* segments_dev;         // [warps + count]
     float* factors_dev;         // [count]
+    Result* result_dev;
     unsigned* ticket_dev;
 };
 
@@ -620,10 +624,11 @@ void free_layout(draco_layout* l) {
     free(l->type);
     free(l->parts);
     if (l->infos_dev) cudaFree(l->infos_dev);
-    if (l->works_dev) cudaFree(l->works_dev);
+    if (l->chunks_dev) cudaFree(l->chunks_dev);
     if (l->slots_dev) cudaFree(l->slots_dev);
     if (l->segments_dev) cudaFree(l->segments_dev);
     if (l->factors_dev) cudaFree(l->factors_dev);
+    if (l->result_dev) cudaFree(l->result_dev);
     if (l->ticket_dev) cudaFree(l->ticket_dev);
     delete l;
 }
@@ -632,36 +637,49 @@ int64_t lines_of(int64_t numel, int per_lane) {            // the first line beg
     return numel ? (numel + per_lane - 1 + 32 * per_lane - 1) / (32 * per_lane) : 0;
 }
 
-// The lines of infos[0 .. count - 1], dealt to warps in contiguous ranges of equal length; returns the number of blocks.
-int deal(const TensorInfo* infos, int count, int by, bool down, int sm_count, WarpWork* works) {
+int64_t lines_of(const TensorInfo* infos, int count, int by) {
     int64_t lines = 0;
     for (int t = 0; t < count; ++t) lines += infos[t].lines[by];
-    const int64_t most = (int64_t)sm_count * kBlocksPerSm, wanted = (lines + kWarps * kMinLines - 1) / (kWarps * kMinLines);
-    const int blocks = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
-    const int warps = blocks * kWarps;
-    const int used = lines < warps ? (int)lines : warps;   // the others have none: every warp between two others has lines
-    auto edge = [&](int w) { return w < used ? lines / used * w + lines % used * w / used : lines; };
-    int t = 0;
-    int64_t before = 0;                                    // lines of the tensors before t
-    for (int w = 0; w < warps; ++w) {
-        const int64_t begin = edge(w), end = edge(w + 1), here = down && end > begin ? end - 1 : begin;
-        while (t < count - 1 && here >= before + infos[t].lines[by]) before += infos[t++].lines[by];
-        works[w] = {down ? end - before : begin - before, infos[t].numel, infos[t].flat, infos[t].lines[by], (int32_t)(end - begin), t, infos[t].type, 0};
-    }
-    return blocks;
+    return lines;
 }
 
-// The segments of infos[0 .. count - 1] by the works of deal(.., down = false): that of warp w and tensor t is number w + t.
-void number_segments(TensorInfo* infos, int count, const WarpWork* works, int warps) {
-    for (int w = 0; w < warps; ++w) {
-        int64_t left = works[w].left, at = works[w].at;
-        for (int t = works[w].tensor; left > 0; ++t, at = 0) {
+// infos[0 .. count - 1] cut into `chunks` chunks of equal length, one line more or less; chunks without a line come last.
+void cut(const TensorInfo* infos, int count, int by, bool down, int chunks, Chunk* table) {
+    const int64_t lines = lines_of(infos, count, by);
+    const int used = lines < chunks ? (int)lines : chunks;
+    auto edge = [&](int c) { return c < used ? lines / used * c + lines % used * c / used : lines; };
+    int t = 0;
+    int64_t before = 0;                                    // lines of the tensors before t
+    for (int c = 0; c < chunks; ++c) {
+        const int64_t begin = edge(c), end = edge(c + 1), here = down && end > begin ? end - 1 : begin;
+        while (t < count - 1 && here >= before + infos[t].lines[by]) before += infos[t++].lines[by];
+        table[c] = {(down ? end : begin) - before, infos[t].numel, infos[t].flat, infos[t].lines[by], (int32_t)(end - begin), t, infos[t].type, 0};
+    }
+}
+
+// The segments of infos[0 .. count - 1] by the chunks of the measurement: that of chunk w and tensor t is number w + t.
+void number_segments(TensorInfo* infos, int count, const Chunk* table, int chunks) {
+    for (int w = 0; w < chunks; ++w) {
+        int64_t left = table[w].left, at = table[w].at;
+        for (int t = table[w].tensor; left > 0; ++t, at = 0) {
             const int64_t take = left < infos[t].lines[BY_BYTES] - at ? left : infos[t].lines[BY_BYTES] - at;
             if (take <= 0) continue;
             if (!infos[t].seg_count++) infos[t].seg_first = w + t;
             left -= take;
         }
     }
+}
+
+// Blocks of a list of so many lines, a chunk a warp.
+int blocks_of(int64_t lines, int what, int sm_count) {
+    auto blocks = [&](int64_t per, int64_t most) {
+        const int64_t wanted = (lines + kWarps * per - 1) / (kWarps * per);
+        return (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
+    };
+    const int64_t wave = (int64_t)sm_count * kBlocksPerSm;
+    const int64_t a_warp = lines / (wave * kWarps);
+    if (what == MEASURE || what == IN_PLACE || a_warp < kWaveLines) return blocks(kMinLines, wave);
+    return blocks(kWavesLines, wave * kWaves);
 }
 
 template <class F>
@@ -672,29 +690,35 @@ int with_capacity(int count, F f) {
 }
 
 template <int N>
-Pointers<N> pointers_of(const void* const* list, const Part& part) {
+Pointers<N> pointers_of(const void* const* list, int count) {
     Pointers<N> p;
-    for (int t = 0; t < part.count; ++t) p.p[t] = const_cast<void*>(list[part.first + t]);
+    for (int t = 0; t < count; ++t) p.p[t] = const_cast<void*>(list[t]);
     return p;
 }
 
-// The block sums of a list, or of the flat vector u (list null); norm: and the norm itself.
-int measure(draco_layout* l, const void* const* list, const float* u, int kind, bool segments, float* norm, cudaStream_t st) {
+int one_wave(const draco_layout* l) { return l->sm_count * kBlocksPerSm; }
+
+// The sums of a list, or of the flat vector u (list null).  segments: of each tensor too.  limit: null (the norm is all that is wanted), or where
+// the next kernel, of later_blocks blocks, gets the factor from.
+int measure(draco_layout* l, const void* const* list, const float* u, int kind, float max_norm, bool segments, float* norm, Limit* limit, int later_blocks,
+            cudaStream_t st) {
     const void* flat[1] = {u};
+    const int blocks = list ? l->all_blocks : l->parts[l->num_parts].blocks[MEASURE];
+    const bool finish = (!limit || later_blocks > one_wave(l)) && !segments;
+    if (limit) *limit = {finish ? l->result_dev : nullptr, static_cast<char*>(l->slots_dev) + (list ? 0 : (size_t)l->all_blocks * 8), blocks, kind, max_norm, norm};
     for (int k = 0; k < (list ? l->num_parts : 1); ++k) {
         const Part& part = l->parts[list ? k : l->num_parts];
-        Part given = part;
-        if (!list) given.first = 0;
-        const int all = list ? l->all_blocks : part.blocks[UP_BYTES], block0 = list ? part.block0 : 0;
+        const int block0 = list ? part.block0 : 0;
         char* slots = static_cast<char*>(l->slots_dev) + (list ? 0 : (size_t)l->all_blocks * 8);
         char* segs = static_cast<char*>(l->segments_dev) + 8 * ((size_t)part.block0 * kWarps + part.first);
         const int rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
-            const Pointers<N> p = pointers_of<N>(list ? list : flat, given);
+            const Pointers<N> p = pointers_of<N>(list ? list + part.first : flat, part.count);
             auto go = [&](auto kernel, auto* slot) {
                 typedef decltype(slot) S;
-                launch_dependent(kernel, dim3(part.blocks[UP_BYTES]), dim3(kThreads), 0, st, p, (const TensorInfo*)l->infos_dev + part.first,
-                                 (const WarpWork*)l->works_dev + part.works[UP_BYTES], (S)slots, block0, (S)segs, norm, all, l->ticket_dev);
+                launch_dependent(kernel, dim3(part.blocks[MEASURE]), dim3(kThreads), 0, st, p, (const TensorInfo*)l->infos_dev + part.first,
+                                 (const Chunk*)l->chunks_dev + part.table[MEASURE], (S)slots, block0, blocks, l->ticket_dev, (S)segs, finish, max_norm, norm,
+                                 limit ? l->result_dev : nullptr);
             };
             if (kind == DRACO_NORM_2) {
                 if (segments) go(measure_kernel<SumSquares, N, true>, (double*)nullptr);
@@ -712,13 +736,13 @@ int measure(draco_layout* l, const void* const* list, const float* u, int kind, 
 }
 
 int finish_each(draco_layout* l, int kind, float max_norm, float* norm, float* each, float* factors, cudaStream_t st) {
-    const dim3 grid(l->count + 1), block(kThreads);
-    if (kind == DRACO_NORM_2)
-        launch_dependent(each_kernel<SumSquares>, grid, block, 0, st, (const TensorInfo*)l->infos_dev, l->count, (const double*)l->segments_dev,
-                         (const double*)l->slots_dev, l->all_blocks, max_norm, norm, each, factors);
-    else
-        launch_dependent(each_kernel<MaxMagnitude>, grid, block, 0, st, (const TensorInfo*)l->infos_dev, l->count,
-                         (const unsigned long long*)l->segments_dev, (const unsigned long long*)l->slots_dev, l->all_blocks, max_norm, norm, each, factors);
+    auto go = [&](auto kernel, auto* slot) {
+        typedef const std::remove_pointer_t<decltype(slot)>* S;
+        launch_dependent(kernel, dim3(l->count + 1), dim3(kThreads), 0, st, (const TensorInfo*)l->infos_dev, (S)l->segments_dev, (S)l->slots_dev, l->all_blocks,
+                         max_norm, norm, each, factors);
+    };
+    if (kind == DRACO_NORM_2) go(each_kernel<SumSquares>, (double*)nullptr);
+    else go(each_kernel<MaxMagnitude>, (unsigned long long*)nullptr);
     DRACO_CUDA(cudaGetLastError());
     return DRACO_OK;
 }
@@ -804,19 +828,17 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
     l->count = count;
     l->size = size;
     l->num_parts = (count + kMaxPointers - 1) / kMaxPointers;
-    int sm_count = 0;
     cudaError_t err = cudaGetDevice(&l->device);
-    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, l->device);
+    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&l->sm_count, cudaDevAttrMultiProcessorCount, l->device);
     if (err != cudaSuccess) { free_layout(l); return cuda_fail(err, "cudaGetDevice"); }
-    const int64_t most_works = (int64_t)(3 * l->num_parts + 1) * sm_count * kBlocksPerSm * kWarps;
     l->numel = static_cast<int64_t*>(malloc(sizeof(int64_t) * count));
     l->type = static_cast<uint8_t*>(malloc(count));
     l->parts = static_cast<Part*>(calloc(l->num_parts + 1, sizeof(Part)));
     TensorInfo* infos = static_cast<TensorInfo*>(calloc(count + 1, sizeof(TensorInfo)));
-    WarpWork* works = static_cast<WarpWork*>(malloc(sizeof(WarpWork) * most_works));
+    Chunk* chunks = nullptr;
+    int64_t num_chunks = 0;
     int rc = DRACO_OK;
-    if (!l->numel || !l->type || !l->parts || !infos || !works) rc = DRACO_ENOMEM;
-    int64_t num_works = 0;
+    if (!l->numel || !l->type || !l->parts || !infos) rc = DRACO_ENOMEM;
     if (rc == DRACO_OK) {
         int64_t flat = 0;
         for (int t = 0; t <= count; ++t) {                 // the last: the flat vector
@@ -837,16 +859,24 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
             p.first = list ? k * kMaxPointers : count;
             p.count = list ? (count - p.first < kMaxPointers ? count - p.first : kMaxPointers) : 1;
             p.block0 = l->all_blocks;
-            for (int way = UP_BYTES; way <= (list ? DOWN_ELEMENTS : UP_BYTES); ++way) {
-                p.works[way] = num_works;
-                p.blocks[way] = deal(infos + p.first, p.count, way == DOWN_ELEMENTS ? BY_ELEMENTS : BY_BYTES, way != UP_BYTES, sm_count, works + num_works);
-                num_works += p.blocks[way] * kWarps;
+            for (int what = MEASURE; what <= (list ? ELEMENTS : MEASURE); ++what) {
+                p.blocks[what] = blocks_of(lines_of(infos + p.first, p.count, what == ELEMENTS ? BY_ELEMENTS : BY_BYTES), what, l->sm_count);
+                p.table[what] = num_chunks;
+                num_chunks += p.blocks[what] * kWarps;
             }
-            if (!list) break;
-            number_segments(infos + p.first, p.count, works + p.works[UP_BYTES], p.blocks[UP_BYTES] * kWarps);
-            for (int t = p.first; t < p.first + p.count; ++t) infos[t].seg_first += p.block0 * kWarps + p.first;
-            l->all_blocks += p.blocks[UP_BYTES];
+            if (list) l->all_blocks += p.blocks[MEASURE];
         }
+        chunks = static_cast<Chunk*>(malloc(sizeof(Chunk) * num_chunks));
+        if (!chunks) rc = DRACO_ENOMEM;
+    }
+    for (int k = 0; k <= l->num_parts && rc == DRACO_OK; ++k) {
+        const Part& p = l->parts[k];
+        TensorInfo* mine = infos + p.first;
+        for (int what = MEASURE; what <= (k < l->num_parts ? ELEMENTS : MEASURE); ++what)
+            cut(mine, p.count, what == ELEMENTS ? BY_ELEMENTS : BY_BYTES, what != MEASURE, p.blocks[what] * kWarps, chunks + p.table[what]);
+        if (k == l->num_parts) break;
+        number_segments(mine, p.count, chunks + p.table[MEASURE], p.blocks[MEASURE] * kWarps);
+        for (int t = 0; t < p.count; ++t) mine[t].seg_first += p.block0 * kWarps + p.first;
     }
 #define DRACO_TRY(call)                                                                          \
     do {                                                                                         \
@@ -855,20 +885,21 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
             if (e__ != cudaSuccess) rc = cuda_fail(e__, #call);                                  \
         }                                                                                        \
     } while (0)
-    const size_t slots = rc == DRACO_OK ? (size_t)l->all_blocks + l->parts[l->num_parts].blocks[UP_BYTES] : 0;
+    const size_t slots = rc == DRACO_OK ? (size_t)l->all_blocks + l->parts[l->num_parts].blocks[MEASURE] : 0;
     DRACO_TRY(cudaMalloc(&l->infos_dev, sizeof(TensorInfo) * (count + 1)));
-    DRACO_TRY(cudaMalloc(&l->works_dev, sizeof(WarpWork) * num_works));
+    DRACO_TRY(cudaMalloc(&l->chunks_dev, sizeof(Chunk) * num_chunks));
     DRACO_TRY(cudaMalloc(&l->slots_dev, 8 * slots));
     DRACO_TRY(cudaMalloc(&l->segments_dev, 8 * (slots * kWarps + count + 1)));
     DRACO_TRY(cudaMalloc(&l->factors_dev, sizeof(float) * count));
+    DRACO_TRY(cudaMalloc(&l->result_dev, sizeof(Result)));
     DRACO_TRY(cudaMalloc(&l->ticket_dev, sizeof(unsigned)));
     DRACO_TRY(cudaMemset(l->ticket_dev, 0, sizeof(unsigned)));
     DRACO_TRY(cudaMemcpy(l->infos_dev, infos, sizeof(TensorInfo) * (count + 1), cudaMemcpyHostToDevice));
-    DRACO_TRY(cudaMemcpy(l->works_dev, works, sizeof(WarpWork) * num_works, cudaMemcpyHostToDevice));
+    DRACO_TRY(cudaMemcpy(l->chunks_dev, chunks, sizeof(Chunk) * num_chunks, cudaMemcpyHostToDevice));
     DRACO_TRY(cudaStreamSynchronize(nullptr));
 #undef DRACO_TRY
     free(infos);
-    free(works);
+    free(chunks);
     if (rc != DRACO_OK) { free_layout(l); return rc; }
     *out = l;
     return DRACO_OK;
@@ -884,9 +915,9 @@ int64_t draco_layout_size(const draco_layout* layout) { return layout ? layout->
 int draco_norm(draco_layout* layout, const void* const* tensors, int kind, float* norm, float* each, void* stream) {
     if (!layout || !addresses_ok(layout, tensors) || !kind_ok(kind) || !norm || !aligned4(norm) || !aligned4(each) || !on_device(layout)) return DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
-    const int rc = measure(layout, tensors, nullptr, kind, each != nullptr, each ? nullptr : norm, st);
+    const int rc = measure(layout, tensors, nullptr, kind, INFINITY, each != nullptr, norm, nullptr, 0, st);
     if (rc != DRACO_OK || !each) return rc;
-    return finish_each(layout, kind, 0.0f, norm, each, nullptr, st);
+    return finish_each(layout, kind, INFINITY, norm, each, nullptr, st);
 }
 
 int draco_clip(draco_layout* layout, const void* const* tensors, void* const* out, int kind, float max_norm, int separately, float* norm, float* each,
@@ -901,16 +932,17 @@ int draco_clip(draco_layout* layout, const void* const* tensors, void* const* ou
     const int alone = distinct(layout, to, tensors);
     if (alone <= 0) return alone < 0 ? alone : DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
-    int rc = measure(layout, tensors, nullptr, kind, separately != 0, nullptr, st);
+    const int table = out ? BYTES : IN_PLACE;
+    Limit limit = {};
+    int rc = measure(layout, tensors, nullptr, kind, max_norm, separately != 0, norm, &limit, layout->parts[0].blocks[table], st);
     if (rc == DRACO_OK && separately) rc = finish_each(layout, kind, max_norm, norm, each, layout->factors_dev, st);
     for (int k = 0; k < layout->num_parts && rc == DRACO_OK; ++k) {
         const Part& part = layout->parts[k];
-        const Limit limit = {layout->slots_dev, layout->all_blocks, kind, max_norm, k == 0 ? norm : nullptr};
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
-            launch_dependent(scale_kernel<N>, dim3(part.blocks[DOWN_BYTES]), dim3(kThreads), 0, st, pointers_of<N>(tensors, part), pointers_of<N>(to, part),
-                             (const TensorInfo*)layout->infos_dev + part.first, (const WarpWork*)layout->works_dev + part.works[DOWN_BYTES], limit,
-                             separately ? (const float*)layout->factors_dev + part.first : nullptr);
+            launch_dependent(scale_kernel<N>, dim3(part.blocks[table]), dim3(kThreads), 0, st, pointers_of<N>(tensors + part.first, part.count), pointers_of<N>(to + part.first, part.count),
+                             (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[table], limit,
+                             separately ? (const float*)layout->factors_dev + part.first : nullptr, !out);
             DRACO_CUDA(cudaGetLastError());
             return DRACO_OK;
         });
@@ -924,14 +956,14 @@ int draco_pack(draco_layout* layout, const void* const* tensors, int kind, float
         return DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
     const bool wanted = norm || !isinf(max_norm);
-    int rc = wanted ? measure(layout, tensors, nullptr, kind, false, nullptr, st) : (int)DRACO_OK;
+    Limit limit = {};
+    int rc = wanted ? measure(layout, tensors, nullptr, kind, max_norm, false, norm, &limit, layout->parts[0].blocks[ELEMENTS], st) : (int)DRACO_OK;
     for (int k = 0; k < layout->num_parts && rc == DRACO_OK; ++k) {
         const Part& part = layout->parts[k];
-        const Limit limit = {wanted ? layout->slots_dev : nullptr, layout->all_blocks, kind, max_norm, k == 0 ? norm : nullptr};
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
-            launch_dependent(pack_kernel<N>, dim3(part.blocks[DOWN_ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(tensors, part),
-                             (const TensorInfo*)layout->infos_dev + part.first, (const WarpWork*)layout->works_dev + part.works[DOWN_ELEMENTS], row, limit);
+            launch_dependent(pack_kernel<N>, dim3(part.blocks[ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(tensors + part.first, part.count),
+                             (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[ELEMENTS], row, limit);
             DRACO_CUDA(cudaGetLastError());
             return DRACO_OK;
         });
@@ -950,16 +982,15 @@ int draco_update(draco_layout* layout, void* const* params, const float* u, floa
     if (alone <= 0) return alone < 0 ? alone : DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
     const bool wanted = norm || !isinf(max_norm);
-    int rc = wanted ? measure(layout, nullptr, u, kind, false, nullptr, st) : (int)DRACO_OK;
+    Limit limit = {};
+    int rc = wanted ? measure(layout, nullptr, u, kind, max_norm, false, norm, &limit, layout->parts[0].blocks[ELEMENTS], st) : (int)DRACO_OK;
     for (int k = 0; k < layout->num_parts && rc == DRACO_OK; ++k) {
         const Part& part = layout->parts[k];
-        const Limit limit = {wanted ? static_cast<char*>(layout->slots_dev) + (size_t)layout->all_blocks * 8 : nullptr,
-                             layout->parts[layout->num_parts].blocks[UP_BYTES], kind, max_norm, k == 0 ? norm : nullptr};
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
             auto go = [&](auto kernel) {
-                launch_dependent(kernel, dim3(part.blocks[DOWN_ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(params, part),
-                                 (const TensorInfo*)layout->infos_dev + part.first, (const WarpWork*)layout->works_dev + part.works[DOWN_ELEMENTS], u, master, scale, limit);
+                launch_dependent(kernel, dim3(part.blocks[ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(params + part.first, part.count),
+                                 (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[ELEMENTS], u, master, scale, limit);
             };
             if (master) go(update_kernel<N, true>);
             else go(update_kernel<N, false>);
