@@ -178,15 +178,20 @@ class _CtypesCalls:
         pass
 
 
+def _load_module(name, path):
+    spec = importlib.util.spec_from_file_location(f"{__package__}.{name}", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
 def _load_native():
     """The module that was built for this interpreter, by its full name; without it ctypes makes the same calls."""
     path = os.path.join(_PKG, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
     if not os.path.exists(path):
         return _CtypesCalls
     try:
-        spec = importlib.util.spec_from_file_location(f"{__package__}._native", path)
-        module = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(module)
+        module = _load_module("_native", path)
     except ImportError as e:
         warnings.warn(f"{path} cannot be loaded ({e}): ctypes makes its calls", RuntimeWarning)
         return _CtypesCalls
@@ -312,12 +317,22 @@ class _Meta(C.Structure):
 _exchange_known = False
 
 
+def _exchange(torch):
+    """What tells the native calls of a tensor: the module that was built for this torch, or else torch's own table of DLPack functions, or None."""
+    path = os.path.join(_PKG, f"_torch_tensors-{torch.__version__}" + sysconfig.get_config_var("EXT_SUFFIX"))
+    if os.path.exists(path):
+        try:
+            return _load_module("_torch_tensors", path).exchange
+        except ImportError as e:
+            warnings.warn(f"{path} cannot be loaded ({e}): torch's own function takes its place", RuntimeWarning)
+    return getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+
+
 def _find_exchange(torch):
-    """torch's table of DLPack functions, where it offers one, for the native calls."""
     global _exchange_known
     if not _exchange_known:
         _exchange_known = True
-        capsule = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+        capsule = _exchange(torch)
         if capsule is not None:
             _native.set_exchange(torch.Tensor, torch.nn.Parameter, capsule)
 

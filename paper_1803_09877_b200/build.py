@@ -1,6 +1,8 @@
 """Builds libdraco.so (sm_100a) in-tree with nvcc.  No JIT, no cache outside the package."""
 from __future__ import annotations
 
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -17,6 +19,19 @@ LIB = os.path.join(PKG, "libdraco.so")
 # The CPython module of the calls that a training loop makes, named after the interpreter that it is built for: another one neither
 # loads it nor takes it for up to date.
 NATIVE = os.path.join(PKG, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
+
+def _torch_tensors() -> tuple[str, str | None]:
+    """The module that reads torch's tensors for the native calls, named after the torch that it is built for as well, and that torch's folder."""
+    try:
+        version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        version = "none"
+    spec = importlib.util.find_spec("torch")
+    folder = os.path.dirname(spec.origin) if spec and spec.origin else None
+    return os.path.join(PKG, f"_torch_tensors-{version}" + sysconfig.get_config_var("EXT_SUFFIX")), folder
+
 
 SOURCES = ["draco_api.cu", "rep_kernels.cu", "cyc_encode.cu", "cyc_locate.cu", "cyc_onepass.cu", "cyc_recover.cu", "harness_kernels.cu",
            "tensor_lists.cu"]
@@ -66,8 +81,18 @@ def build(force: bool = False, verbose: bool = False) -> str:
         run([nvcc, "-shared", "-o", LIB] + objs + ["-lcudart"])
     src = os.path.join(CSRC, "native.cpp")
     python_include = sysconfig.get_paths()["include"]
-    if force or _stale(NATIVE, [src, headers[0]]):
-        if os.path.exists(os.path.join(python_include, "Python.h")):
+    beside = os.path.join(CSRC, "dlpack_tensor.h")
+    has_python = os.path.exists(os.path.join(python_include, "Python.h"))
+    tensors, torch = _torch_tensors()
+    if torch and has_python and (force or _stale(tensors, [os.path.join(CSRC, "torch_tensors.cpp"), beside])):
+        try:
+            run([nvcc, "-shared", "-O2", "-std=c++17", "-Xcompiler", "-fPIC", "-I", os.path.join(torch, "include"), "-I",
+                 os.path.join(torch, "include", "torch", "csrc", "api", "include"), "-I", CSRC, "-I", python_include,
+                 os.path.join(CSRC, "torch_tensors.cpp"), "-o", tensors, "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+        except RuntimeError as e:
+            sys.stderr.write(f"{os.path.basename(tensors)} is not built, torch's own function takes its place: {str(e)[:400]}\n")
+    if force or _stale(NATIVE, [src, headers[0], beside]):
+        if has_python:
             run([nvcc, "-shared", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", python_include, src,
                  "-o", NATIVE, "-L", PKG, "-Xlinker", "-l:libdraco.so", "-Xlinker", "-rpath=$ORIGIN"])
         else:

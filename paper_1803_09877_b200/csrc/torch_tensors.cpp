@@ -1,0 +1,46 @@
+// What native.cpp asks of a tensor (address, device, type, sizes, strides), read from torch's C++ object: about 15 ns, where torch's own DLPack
+// function takes 56.  Built for one version of torch and named after it; without it the calls go through torch's function.
+#define PY_SSIZE_T_CLEAN
+#include <torch/csrc/autograd/python_variable.h>
+
+#include "dlpack_tensor.h"
+
+namespace {
+
+int tensor_from_object(void* object, DLTensor* out) {
+    try {
+        const at::Tensor& t = THPVariable_Unpack(static_cast<PyObject*>(object));
+        if (!t.defined() || t.layout() != at::kStrided || t.is_neg()) return -1;
+        constexpr int32_t kCpu = 1, kCuda = 2;
+        out->device = {t.is_cuda() ? kCuda : kCpu, t.is_cuda() ? (int32_t)t.get_device() : 0};
+        switch (t.scalar_type()) {
+            case at::kFloat: out->dtype = {2, 32, 1}; break;
+            case at::kBFloat16: out->dtype = {4, 16, 1}; break;
+            case at::kHalf: out->dtype = {2, 16, 1}; break;
+            default: return -1;
+        }
+        out->data = const_cast<void*>(t.const_data_ptr());
+        out->byte_offset = 0;
+        out->ndim = (int32_t)t.dim();
+        out->shape = const_cast<int64_t*>(t.sizes().data());
+        out->strides = const_cast<int64_t*>(t.strides().data());
+        return 0;
+    } catch (...) {
+        return -1;
+    }
+}
+
+DLPackExchangeAPI api = {1, 3, nullptr, nullptr, nullptr, nullptr, tensor_from_object, nullptr};
+
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_tensors", nullptr, -1, nullptr, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__torch_tensors(void) {
+    PyObject* m = PyModule_Create(&module);
+    PyObject* capsule = m ? PyCapsule_New(&api, "dlpack_exchange_api", nullptr) : nullptr;
+    if (capsule && PyModule_AddObject(m, "exchange", capsule) == 0) return m;
+    Py_XDECREF(capsule);
+    Py_XDECREF(m);
+    return nullptr;
+}
