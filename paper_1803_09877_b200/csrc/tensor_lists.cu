@@ -10,6 +10,7 @@
 // what it holds.  The ranges depend on sizes alone and are made once, with the layout; the tensors' addresses come with every call, as
 // kernel parameters (a graph captures them, nothing is uploaded), at most kMaxPointers a launch; longer lists take several launches.
 // No warp waits for another: block sums are written out and added up, in a fixed order, by whoever needs the norm next.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -29,13 +30,16 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kBlocksPerSm = 4;
 constexpr int kMaxPointers = 2000;                // two lists of 8-byte pointers within the 32,764 bytes of kernel parameters
 constexpr int64_t kMostElements = (int64_t)1 << 40; // a warp counts its lines and their elements in 32 bits
-constexpr int kMinLines = 8;                      // a warp's, before the list gets another one
+constexpr int kMinLines = 4;                      // a warp's, before the list gets another one
+constexpr int kVisit = 8;
 // Second passes of long lists: several waves of blocks with short chunks.  SMs that are further from memory take longer over the same share, and
 // with one wave the last of them holds the others up (138 M bf16 packed: one wave 201 us, chunks of 24 lines 185, of 12 182, of 8 181; with a
 // master copy updated, 60.2 M 186, 176, 173, 171).  Below kWaveLines lines a warp one wave is level or faster.
 constexpr int kWaveLines = 32, kWavesLines = 8, kWaves = 64;
 // In place most calls have nothing to write, and blocks that only find that out cost 1.2 us a thousand: always one wave (1.0e9 bf16 below the limit
 // 296 us, chunks of 64 lines 306, of 8 346; above it 966, 925, 901).
+// A list of up to kSmallTensors tensors and so many lines is left to one cluster of blocks.
+constexpr int kSmallTensors = 512, kSmallBlocks = 16, kSmallLines = 8;
 constexpr int kBatch = 8;                         // lines that a warp loads at once
 
 // Lines: 512 bytes of a tensor's own type (one 16-byte word a lane) where the tensor alone is walked, 128 elements (four a lane) where
@@ -458,20 +462,30 @@ __device__ __forceinline__ void scale_lines(const void* from, void* to, int64_t 
     range.ends([&](int i) { q[i] = Elements<TYPE>::round(Elements<TYPE>::value(p[i]) * c); });
 }
 
-// to = from * c.  In place nothing is written where c is 1.
+// to = from * c, c the factor of all or (factors) of each tensor.  In place nothing is written where c is 1.
+template <int N>
+__device__ __forceinline__ void scale_chunk(const Pointers<N>& from, const Pointers<N>& to, const TensorInfo* infos, const Chunk& chunk, float all,
+                                            const float* factors) {
+    walk<true, BY_BYTES>(infos, chunk, [&](int t, int type_, int64_t, int64_t numel, int64_t line, int take) {
+        const float c = factors ? __ldcg(factors + t) : all;
+        if (!from.p[t] || (c == 1.0f && from.p[t] == to.p[t])) return;
+        by_type(type_, [&](auto type) { scale_lines<decltype(type)::value>(from.p[t], to.p[t], numel, line, take, c); });
+    });
+}
+
+__device__ __forceinline__ Chunk chunk_from_the_end(const Chunk* __restrict__ chunks) {
+    return chunks[(gridDim.x - 1 - blockIdx.x) * kWarps + (threadIdx.x >> 5)];
+}
+
 template <int N>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
 scale_kernel(const __grid_constant__ Pointers<N> from, const __grid_constant__ Pointers<N> to, const TensorInfo* __restrict__ infos,
              const Chunk* __restrict__ chunks, Limit limit, const float* factors, bool in_place) {
-    const Chunk chunk = chunks[(gridDim.x - 1 - blockIdx.x) * kWarps + (threadIdx.x >> 5)];
+    const Chunk chunk = chunk_from_the_end(chunks);
     pdl_begin();
     const float all = factors ? 1.0f : factor(limit).c;
     if (in_place && !factors && all == 1.0f) return;
-    walk<true, BY_BYTES>(infos, chunk, [&](int t, int type_, int64_t, int64_t numel, int64_t line, int take) {
-        const float c = factors ? factors[t] : all;
-        if (!from.p[t] || (c == 1.0f && from.p[t] == to.p[t])) return;
-        by_type(type_, [&](auto type) { scale_lines<decltype(type)::value>(from.p[t], to.p[t], numel, line, take, c); });
-    });
+    scale_chunk<N>(from, to, infos, chunk, all, factors);
 }
 
 // ---- a tensor beside its part of a flat fp32 vector: four elements a lane ----
@@ -510,11 +524,7 @@ __device__ __forceinline__ void pack_lines(const void* base, float* out, int64_t
 
 // row[flat + i] = c * tensor[i]; zeros for a tensor that is absent.
 template <int N>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
-pack_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks, float* row, Limit limit) {
-    const Chunk chunk = chunks[(gridDim.x - 1 - blockIdx.x) * kWarps + (threadIdx.x >> 5)];
-    pdl_begin();
-    const float c = factor(limit).c;
+__device__ __forceinline__ void pack_chunk(const Pointers<N>& list, const TensorInfo* infos, const Chunk& chunk, float* row, float c) {
     walk<true, BY_ELEMENTS>(infos, chunk, [&](int t, int type_, int64_t flat, int64_t numel, int64_t line, int take) {
         if (list.p[t]) {
             by_type(type_, [&](auto type) { pack_lines<decltype(type)::value>(list.p[t], row + flat, numel, line, take, c); });
@@ -530,6 +540,14 @@ pack_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restri
         });
         range.ends([&](int i) { q[i] = 0.0f; });
     });
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+pack_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks, float* row, Limit limit) {
+    const Chunk chunk = chunk_from_the_end(chunks);
+    pdl_begin();
+    pack_chunk<N>(list, infos, chunk, row, factor(limit).c);
 }
 
 // The groups of four are those of the side that is both read and written: w, or the master copy of it.
@@ -577,17 +595,132 @@ __device__ __forceinline__ void update_lines(void* base, const float* u, float* 
 
 // w <- w - scale c u; MASTER: the fp32 master copy instead, and w is that, rounded.  Nothing where |u| is not finite.
 template <int N, bool MASTER>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
-update_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks,
-              const float* __restrict__ u, float* __restrict__ master, float scale, Limit limit) {
-    const Chunk chunk = chunks[(gridDim.x - 1 - blockIdx.x) * kWarps + (threadIdx.x >> 5)];
-    pdl_begin();
-    const Result r = factor(limit);
+__device__ __forceinline__ void update_chunk(const Pointers<N>& list, const TensorInfo* infos, const Chunk& chunk, const float* u, float* master, float scale,
+                                             const Result& r) {
     if (!r.finite) return;
     const float s = scale * r.c;
     walk<true, BY_ELEMENTS>(infos, chunk, [&](int t, int type_, int64_t flat, int64_t numel, int64_t line, int take) {
         if (list.p[t]) by_type(type_, [&](auto type) { update_lines<decltype(type)::value, MASTER>(list.p[t], u, master, flat, numel, line, take, s); });
     });
+}
+
+template <int N, bool MASTER>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+update_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks,
+              const float* __restrict__ u, float* __restrict__ master, float scale, Limit limit) {
+    const Chunk chunk = chunk_from_the_end(chunks);
+    pdl_begin();
+    update_chunk<N, MASTER>(list, infos, chunk, u, master, scale, factor(limit));
+}
+
+// ---- short lists: measured and worked on by one cluster, in one launch ----
+
+// The blocks of a cluster exchange their sums through shared memory, behind the hardware's barrier; the second pass finds its lines in L1.
+struct Small {
+    float max_norm;
+    float* norm;           // may be null
+    float* each;           // may be null
+    void* segments;        // null: one factor for all
+    float* factors;
+};
+
+template <class K>
+__device__ __forceinline__ Result cluster_total(typename K::Slot acc, const Small& s) {
+    __shared__ typename K::Slot shared[kWarps], mine;
+    auto cluster = cooperative_groups::this_cluster();
+    acc = block_total<K>(acc, shared);
+    if (threadIdx.x == 0) mine = acc;
+    cluster.sync();
+    typename K::Slot a = K::zero();
+    for (int r = 0; r < (int)cluster.num_blocks(); ++r) K::add(a, *cluster.map_shared_rank(&mine, r));
+    const double n = K::norm(a);
+    if (s.norm && blockIdx.x == 0 && threadIdx.x == 0) *s.norm = (float)n;
+    return result_of(n, s.max_norm);
+}
+
+// This warp's part of a measurement; with segments the factors of the tensors, too, are in place when it returns.
+template <class K, int N>
+__device__ __forceinline__ Result measure_small(const Pointers<N>& list, const TensorInfo* infos, const Chunk& chunk, int count, const Small& s) {
+    typedef typename K::Slot Slot;
+    Slot acc = K::zero();
+    const int w = blockIdx.x * kWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    Slot* segments = static_cast<Slot*>(s.segments);
+    walk<false, BY_BYTES>(infos, chunk, [&](int t, int type_, int64_t, int64_t numel, int64_t line, int take) {
+        Slot a = K::zero();
+        if (list.p[t]) by_type(type_, [&](auto type) { measure_lines<K, decltype(type)::value>(list.p[t], numel, line, take, a); });
+        if (segments) {
+            const Slot total = warp_total<K>(a);
+            if (lane == 0) segments[w + t] = total;
+        }
+        K::add(acc, a);
+    });
+    const Result r = cluster_total<K>(acc, s);
+    if (!segments) return r;
+    for (int t = w; t < count; t += gridDim.x * kWarps) {
+        const int first = infos[t].seg_first, n = infos[t].seg_count;
+        Slot a = K::zero();
+        for (int i = lane; i < n; i += 32) K::add(a, __ldcg(segments + first + i));
+        const double norm = K::norm(warp_total<K>(a));
+        if (lane == 0) {
+            if (s.each) s.each[t] = (float)norm;
+            s.factors[t] = result_of(norm, s.max_norm).c;
+        }
+    }
+    cooperative_groups::this_cluster().sync();
+    return r;
+}
+
+// No block leaves while another may still read its sum.
+struct Leave {
+    __device__ Leave() { cooperative_groups::this_cluster().barrier_arrive(); }
+    __device__ ~Leave() { cooperative_groups::this_cluster().barrier_wait(); }
+};
+
+template <class K, int N>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+small_norm_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks, int count, Small s) {
+    const Chunk chunk = chunks[blockIdx.x * kWarps + (threadIdx.x >> 5)];
+    pdl_begin();
+    measure_small<K, N>(list, infos, chunk, count, s);
+    const Leave leave;
+}
+
+template <class K, int N>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+small_scale_kernel(const __grid_constant__ Pointers<N> from, const __grid_constant__ Pointers<N> to, const TensorInfo* __restrict__ infos,
+                   const Chunk* __restrict__ chunks, const Chunk* __restrict__ second, int count, Small s) {
+    const int w = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const Chunk chunk = chunks[w], back = second[w];
+    pdl_begin();
+    const Result r = measure_small<K, N>(from, infos, chunk, count, s);
+    const Leave leave;
+    scale_chunk<N>(from, to, infos, back, r.c, s.segments ? s.factors : nullptr);
+}
+
+template <class K, int N>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+small_pack_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks,
+                  const Chunk* __restrict__ second, float* row, Small s) {
+    const int w = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const Chunk chunk = chunks[w], back = second[w];
+    pdl_begin();
+    const Result r = measure_small<K, N>(list, infos, chunk, 0, s);
+    const Leave leave;
+    pack_chunk<N>(list, infos, back, row, r.c);
+}
+
+template <class K, int N, bool MASTER>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+small_update_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ flat,
+                    const Chunk* __restrict__ second, const float* __restrict__ u, float* __restrict__ master, float scale, Small s) {
+    const int w = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const Chunk chunk = flat[w], back = second[w];
+    pdl_begin();
+    typename K::Slot acc = K::zero();
+    if (chunk.left > 0) measure_lines<K, DRACO_F32>(u, chunk.numel, chunk.at, chunk.left, acc);
+    const Result r = cluster_total<K>(acc, s);
+    const Leave leave;
+    update_chunk<N, MASTER>(list, infos, back, u, master, scale, r);
 }
 
 #undef DRACO_WHOLE
@@ -607,6 +740,7 @@ struct draco_layout {
     int num_parts;
     int all_blocks;
     int sm_count;
+    int small;                  // blocks of the cluster that does all of a call, or 0
     TensorInfo* infos_dev;      // [count], then the flat vector's
     Chunk* chunks_dev;
     void* slots_dev;            // [all_blocks], then [blocks of the flat vector]; 8 bytes each
@@ -637,23 +771,42 @@ int64_t lines_of(int64_t numel, int per_lane) {            // the first line beg
     return numel ? (numel + per_lane - 1 + 32 * per_lane - 1) / (32 * per_lane) : 0;
 }
 
-int64_t lines_of(const TensorInfo* infos, int count, int by) {
-    int64_t lines = 0;
-    for (int t = 0; t < count; ++t) lines += infos[t].lines[by];
-    return lines;
+// What a list costs, in lines: a tensor that a warp comes to costs it as much time as kVisit lines, the wait for its first ones.
+int64_t cost_of(const TensorInfo* infos, int count, int by) {
+    int64_t cost = 0;
+    for (int t = 0; t < count; ++t) cost += infos[t].lines[by] ? infos[t].lines[by] + kVisit : 0;
+    return cost;
 }
 
-// infos[0 .. count - 1] cut into `chunks` chunks of equal length, one line more or less; chunks without a line come last.
+// infos[0 .. count - 1] cut into `chunks` chunks of equal cost.
 void cut(const TensorInfo* infos, int count, int by, bool down, int chunks, Chunk* table) {
-    const int64_t lines = lines_of(infos, count, by);
-    const int used = lines < chunks ? (int)lines : chunks;
-    auto edge = [&](int c) { return c < used ? lines / used * c + lines % used * c / used : lines; };
-    int t = 0;
-    int64_t before = 0;                                    // lines of the tensors before t
+    const int64_t cost = cost_of(infos, count, by);
+    const int used = cost < chunks ? (int)cost : chunks;   // the others, the last ones, have none: every chunk between two of a tensor has lines of it
+    struct Place {
+        int t;
+        int64_t before;                                    // cost of the tensors before t
+        int64_t line;                                      // in t
+    } begin = {0, 0, 0};
+    auto next = [&](Place p, int64_t at) {
+        auto of = [&](int t) { return infos[t].lines[by] ? infos[t].lines[by] + kVisit : 0; };
+        while (p.t < count - 1 && at >= p.before + of(p.t)) p.before += of(p.t++);
+        p.line = at - p.before - kVisit;
+        if (p.line < 0) p.line = 0;
+        if (p.line > infos[p.t].lines[by]) p.line = infos[p.t].lines[by];
+        return p;
+    };
+    begin = next(begin, 0);
     for (int c = 0; c < chunks; ++c) {
-        const int64_t begin = edge(c), end = edge(c + 1), here = down && end > begin ? end - 1 : begin;
-        while (t < count - 1 && here >= before + infos[t].lines[by]) before += infos[t++].lines[by];
-        table[c] = {(down ? end : begin) - before, infos[t].numel, infos[t].flat, infos[t].lines[by], (int32_t)(end - begin), t, infos[t].type, 0};
+        const Place end = next(begin, c + 1 < used ? cost / used * (c + 1) + cost % used * (c + 1) / used : cost);
+        int64_t left = end.line - begin.line;
+        for (int t = begin.t; t < end.t; ++t) left += infos[t].lines[by];
+        Place from = begin;
+        if (down) {                                        // the tensor that holds the last line
+            from = end;
+            while (from.line == 0 && from.t > begin.t) from.line = infos[--from.t].lines[by];
+        }
+        table[c] = {from.line, infos[from.t].numel, infos[from.t].flat, infos[from.t].lines[by], (int32_t)left, from.t, infos[from.t].type, 0};
+        begin = end;
     }
 }
 
@@ -670,14 +823,15 @@ void number_segments(TensorInfo* infos, int count, const Chunk* table, int chunk
     }
 }
 
-// Blocks of a list of so many lines, a chunk a warp.
-int blocks_of(int64_t lines, int what, int sm_count) {
+// Blocks of a list of this cost, a chunk a warp.
+int blocks_of(int64_t cost, int what, int sm_count, int small) {
+    if (small) return small;
     auto blocks = [&](int64_t per, int64_t most) {
-        const int64_t wanted = (lines + kWarps * per - 1) / (kWarps * per);
+        const int64_t wanted = (cost + kWarps * per - 1) / (kWarps * per);
         return (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
     };
     const int64_t wave = (int64_t)sm_count * kBlocksPerSm;
-    const int64_t a_warp = lines / (wave * kWarps);
+    const int64_t a_warp = cost / (wave * kWarps);
     if (what == MEASURE || what == IN_PLACE || a_warp < kWaveLines) return blocks(kMinLines, wave);
     return blocks(kWavesLines, wave * kWaves);
 }
@@ -804,6 +958,50 @@ int distinct(const draco_layout* l, const void* const* to, const void* const* fr
     return ok;
 }
 
+template <class F>
+int with_small_capacity(int count, F f) {
+    if (count <= 64) return f(std::integral_constant<int, 64>());
+    return f(std::integral_constant<int, kSmallTensors>());
+}
+
+template <class F>
+int with_kind(int kind, F f) {
+    return kind == DRACO_NORM_2 ? f(SumSquares()) : f(MaxMagnitude());
+}
+
+// launch_dependent with all blocks in one cluster.
+template <typename... Params, typename... Args>
+int launch_small(const draco_layout* l, void (*kernel)(Params...), cudaStream_t st, Args... args) {
+    cudaLaunchAttribute attrs[2] = {};
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = l->small;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(l->small);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = st;
+    cfg.attrs = attrs;
+    cfg.numAttrs = 2;
+    DRACO_CUDA(cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...));
+    return DRACO_OK;
+}
+
+// Clusters of more than eight blocks have to be allowed, kernel by kernel and device by device.
+template <class K, int N>
+cudaError_t allow_large_clusters() {
+    const void* kernels[] = {(const void*)small_norm_kernel<K, N>, (const void*)small_scale_kernel<K, N>, (const void*)small_pack_kernel<K, N>,
+                             (const void*)small_update_kernel<K, N, false>, (const void*)small_update_kernel<K, N, true>};
+    for (const void* k : kernels) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+const Chunk* table_of(const draco_layout* l, int what) { return l->chunks_dev + l->parts[0].table[what]; }
+
 bool kind_ok(int kind) { return kind == DRACO_NORM_2 || kind == DRACO_NORM_MAX; }
 
 }  // namespace
@@ -853,6 +1051,11 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
             l->type[t] = (uint8_t)i.type;
             flat += i.numel;
         }
+        const int64_t alone = cost_of(infos, count, BY_BYTES), beside = cost_of(infos, count, BY_ELEMENTS), most = alone > beside ? alone : beside;
+        if (count <= kSmallTensors && most <= kSmallBlocks * kWarps * kSmallLines) {
+            const int64_t wanted = (most + kWarps * kMinLines - 1) / (kWarps * kMinLines);
+            l->small = (int)(wanted < 1 ? 1 : wanted < kSmallBlocks ? wanted : kSmallBlocks);
+        }
         for (int k = 0; k <= l->num_parts; ++k) {
             Part& p = l->parts[k];
             const bool list = k < l->num_parts;
@@ -860,7 +1063,7 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
             p.count = list ? (count - p.first < kMaxPointers ? count - p.first : kMaxPointers) : 1;
             p.block0 = l->all_blocks;
             for (int what = MEASURE; what <= (list ? ELEMENTS : MEASURE); ++what) {
-                p.blocks[what] = blocks_of(lines_of(infos + p.first, p.count, what == ELEMENTS ? BY_ELEMENTS : BY_BYTES), what, l->sm_count);
+                p.blocks[what] = blocks_of(cost_of(infos + p.first, p.count, what == ELEMENTS ? BY_ELEMENTS : BY_BYTES), what, l->sm_count, l->small);
                 p.table[what] = num_chunks;
                 num_chunks += p.blocks[what] * kWarps;
             }
@@ -897,6 +1100,14 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
     DRACO_TRY(cudaMemcpy(l->infos_dev, infos, sizeof(TensorInfo) * (count + 1), cudaMemcpyHostToDevice));
     DRACO_TRY(cudaMemcpy(l->chunks_dev, chunks, sizeof(Chunk) * num_chunks, cudaMemcpyHostToDevice));
     DRACO_TRY(cudaStreamSynchronize(nullptr));
+    if (l->small > 8) {
+        with_small_capacity(count, [&](auto n) {
+            constexpr int N = decltype(n)::value;
+            DRACO_TRY((allow_large_clusters<SumSquares, N>()));
+            DRACO_TRY((allow_large_clusters<MaxMagnitude, N>()));
+            return 0;
+        });
+    }
 #undef DRACO_TRY
     free(infos);
     free(chunks);
@@ -915,6 +1126,15 @@ int64_t draco_layout_size(const draco_layout* layout) { return layout ? layout->
 int draco_norm(draco_layout* layout, const void* const* tensors, int kind, float* norm, float* each, void* stream) {
     if (!layout || !addresses_ok(layout, tensors) || !kind_ok(kind) || !norm || !aligned4(norm) || !aligned4(each) || !on_device(layout)) return DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
+    if (layout->small)
+        return with_small_capacity(layout->count, [&](auto n) {
+            return with_kind(kind, [&](auto k) {
+                constexpr int N = decltype(n)::value;
+                const Small s = {INFINITY, norm, each, each ? layout->segments_dev : nullptr, layout->factors_dev};
+                return launch_small(layout, small_norm_kernel<decltype(k), N>, st, pointers_of<N>(tensors, layout->count), layout->infos_dev,
+                                    table_of(layout, MEASURE), layout->count, s);
+            });
+        });
     const int rc = measure(layout, tensors, nullptr, kind, INFINITY, each != nullptr, norm, nullptr, 0, st);
     if (rc != DRACO_OK || !each) return rc;
     return finish_each(layout, kind, INFINITY, norm, each, nullptr, st);
@@ -933,6 +1153,15 @@ int draco_clip(draco_layout* layout, const void* const* tensors, void* const* ou
     if (alone <= 0) return alone < 0 ? alone : DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
     const int table = out ? BYTES : IN_PLACE;
+    if (layout->small)
+        return with_small_capacity(layout->count, [&](auto n) {
+            return with_kind(kind, [&](auto k) {
+                constexpr int N = decltype(n)::value;
+                const Small s = {max_norm, norm, each, separately ? layout->segments_dev : nullptr, layout->factors_dev};
+                return launch_small(layout, small_scale_kernel<decltype(k), N>, st, pointers_of<N>(tensors, layout->count),
+                                    pointers_of<N>(to, layout->count), layout->infos_dev, table_of(layout, MEASURE), table_of(layout, table), layout->count, s);
+            });
+        });
     Limit limit = {};
     int rc = measure(layout, tensors, nullptr, kind, max_norm, separately != 0, norm, &limit, layout->parts[0].blocks[table], st);
     if (rc == DRACO_OK && separately) rc = finish_each(layout, kind, max_norm, norm, each, layout->factors_dev, st);
@@ -956,6 +1185,14 @@ int draco_pack(draco_layout* layout, const void* const* tensors, int kind, float
         return DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
     const bool wanted = norm || !isinf(max_norm);
+    if (layout->small && wanted)
+        return with_small_capacity(layout->count, [&](auto n) {
+            return with_kind(kind, [&](auto k) {
+                constexpr int N = decltype(n)::value;
+                return launch_small(layout, small_pack_kernel<decltype(k), N>, st, pointers_of<N>(tensors, layout->count), layout->infos_dev,
+                                    table_of(layout, MEASURE), table_of(layout, ELEMENTS), row, Small{max_norm, norm, nullptr, nullptr, nullptr});
+            });
+        });
     Limit limit = {};
     int rc = wanted ? measure(layout, tensors, nullptr, kind, max_norm, false, norm, &limit, layout->parts[0].blocks[ELEMENTS], st) : (int)DRACO_OK;
     for (int k = 0; k < layout->num_parts && rc == DRACO_OK; ++k) {
@@ -982,6 +1219,18 @@ int draco_update(draco_layout* layout, void* const* params, const float* u, floa
     if (alone <= 0) return alone < 0 ? alone : DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
     const bool wanted = norm || !isinf(max_norm);
+    if (layout->small && wanted)
+        return with_small_capacity(layout->count, [&](auto n) {
+            return with_kind(kind, [&](auto k) -> int {
+                constexpr int N = decltype(n)::value;
+                auto go = [&](auto kernel) {
+                    return launch_small(layout, kernel, st, pointers_of<N>(params, layout->count), layout->infos_dev,
+                                        layout->chunks_dev + layout->parts[layout->num_parts].table[MEASURE], table_of(layout, ELEMENTS), u, master, scale,
+                                        Small{max_norm, norm, nullptr, nullptr, nullptr});
+                };
+                return master ? go(small_update_kernel<decltype(k), N, true>) : go(small_update_kernel<decltype(k), N, false>);
+            });
+        });
     Limit limit = {};
     int rc = wanted ? measure(layout, nullptr, u, kind, max_norm, false, norm, &limit, layout->parts[0].blocks[ELEMENTS], st) : (int)DRACO_OK;
     for (int k = 0; k < layout->num_parts && rc == DRACO_OK; ++k) {
