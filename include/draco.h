@@ -273,8 +273,8 @@ int draco_corrupt(const draco_plan* plan, void* R, const int* adv_idx, const int
  * These calls stand between the two: norms and clipping of a list, a list packed into a row of G for draco_encode, and the decoded
  * sum applied to a list of parameters.  (The paper has no counterpart: its model is one vector.)
  *
- * A layout holds the sizes and types of one list, the split of the work, and scratch for partial sums (8 bytes a warp, at most 300 KB,
- * and 60 bytes a tensor).  Tensor t takes entries off_t .. off_t + numel[t] - 1 of the flat vector, off_t = numel[0] + .. + numel[t-1];
+ * A layout holds the sizes and types of one list, the split of the work over warps (48 bytes for every 4 KB of a long list, at most 30 MB)
+ * and scratch for partial sums (at most 200 KB and 80 bytes a tensor), all in device memory that draco_layout_create allocates.  Tensor t takes entries off_t .. off_t + numel[t] - 1 of the flat vector, off_t = numel[0] + .. + numel[t-1];
  * d = their sum (draco_layout_size).  Each call takes the list as a host array of device addresses, read before the call returns.
  * Tensors are dense (numel contiguous elements); an address needs the alignment of its element only.  NULL: the tensor is absent (a
  * parameter without a gradient).  Sizes of zero are allowed.  The rows of G are such a list too.

@@ -988,7 +988,9 @@ int launch_small(const draco_layout* l, void (*kernel)(Params...), cudaStream_t 
     return DRACO_OK;
 }
 
-// Clusters of more than eight blocks have to be allowed, kernel by kernel and device by device.
+constexpr int kPortable = 8;                               // blocks of a cluster that every device takes
+
+// Larger clusters have to be allowed, kernel by kernel and device by device.
 template <class K, int N>
 cudaError_t allow_large_clusters() {
     const void* kernels[] = {(const void*)small_norm_kernel<K, N>, (const void*)small_scale_kernel<K, N>, (const void*)small_pack_kernel<K, N>,
@@ -998,6 +1000,26 @@ cudaError_t allow_large_clusters() {
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
+}
+
+bool large_cluster_fits(int count, int blocks) {
+    return with_small_capacity(count, [&](auto n) -> int {
+        constexpr int N = decltype(n)::value;
+        if (allow_large_clusters<SumSquares, N>() != cudaSuccess || allow_large_clusters<MaxMagnitude, N>() != cudaSuccess) return 0;
+        cudaLaunchAttribute attr = {};
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = blocks;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(blocks);
+        cfg.blockDim = dim3(kThreads);
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        int clusters = 0;
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(&clusters, small_scale_kernel<SumSquares, N>, &cfg);
+        if (e != cudaSuccess) cudaGetLastError();
+        return e == cudaSuccess && clusters > 0;
+    });
 }
 
 const Chunk* table_of(const draco_layout* l, int what) { return l->chunks_dev + l->parts[0].table[what]; }
@@ -1055,6 +1077,7 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
         if (count <= kSmallTensors && most <= kSmallBlocks * kWarps * kSmallLines) {
             const int64_t wanted = (most + kWarps * kMinLines - 1) / (kWarps * kMinLines);
             l->small = (int)(wanted < 1 ? 1 : wanted < kSmallBlocks ? wanted : kSmallBlocks);
+            if (l->small > kPortable && !large_cluster_fits(count, l->small)) l->small = kPortable;
         }
         for (int k = 0; k <= l->num_parts; ++k) {
             Part& p = l->parts[k];
@@ -1100,14 +1123,6 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
     DRACO_TRY(cudaMemcpy(l->infos_dev, infos, sizeof(TensorInfo) * (count + 1), cudaMemcpyHostToDevice));
     DRACO_TRY(cudaMemcpy(l->chunks_dev, chunks, sizeof(Chunk) * num_chunks, cudaMemcpyHostToDevice));
     DRACO_TRY(cudaStreamSynchronize(nullptr));
-    if (l->small > 8) {
-        with_small_capacity(count, [&](auto n) {
-            constexpr int N = decltype(n)::value;
-            DRACO_TRY((allow_large_clusters<SumSquares, N>()));
-            DRACO_TRY((allow_large_clusters<MaxMagnitude, N>()));
-            return 0;
-        });
-    }
 #undef DRACO_TRY
     free(infos);
     free(chunks);

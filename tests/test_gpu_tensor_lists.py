@@ -92,6 +92,10 @@ LISTS = {
     "mixed": (EDGES + [70_001, 5], (["bf16", "f32", "f16"] * 7)[: len(EDGES) + 2]),
     "large": ([3_000_001, 64, 2_500_000], ["bf16", "f32", "f32"]),
     "hundred": ([37 * (i % 5) + i for i in range(100)], ["f16", "f32"] * 50),
+    # beyond what one cluster takes
+    "long_f32": (EDGES + [400_003], ["f32"] * (len(EDGES) + 1)),
+    "long_bf16": ([900_001] + EDGES, ["bf16"] * (len(EDGES) + 1)),
+    "long_mixed": (EDGES + [300_007, 250_001, 9], (["f16", "f32", "bf16"] * 8)[: len(EDGES) + 3]),
     "thousand": ([257 + 64 * (i % 3) for i in range(1000)], ["bf16"] * 1000),
     "many": ([i % 7 for i in range(4500)], ["f32", "bf16", "f16"] * 1500),
 }
@@ -277,8 +281,9 @@ def test_norms_of_extreme_values(t, value, shift):
 @pytest.mark.parametrize("kind", ["2", "max"])
 @pytest.mark.parametrize("t", sorted(TYPES))
 @pytest.mark.parametrize("at", [0, 5, 2500, -1])
-def test_a_norm_that_is_not_finite_bounds_nothing(t, kind, bad, at):
-    sizes, types = [3, 5001, 64], [t] * 3
+@pytest.mark.parametrize("n", [5001, 700_001])
+def test_a_norm_that_is_not_finite_bounds_nothing(t, kind, bad, at, n):
+    sizes, types = [3, n, 64], [t] * 3
     l = List(sizes, types, [0, 1], seed=16)
     l.tensors[1][at] = bad
     before, lay, norm = l.bits(), _layout(l), torch.zeros(1, device="cuda")
@@ -430,6 +435,62 @@ def test_two_lists_on_two_streams():
         _scaled_ok(r[:lay.d].double().cpu().numpy(), np.concatenate(l.wide()), 1.0 / v, "f32", 6 * U)
 
 
+@pytest.mark.parametrize("n", [40, 4_000_000])
+def test_a_layouts_first_calls_captured(n):
+    """Nothing that a call needs is made, loaded or allocated by an earlier one."""
+    code = f"""
+import torch, paper_1803_09877_b200 as dr
+x, w = torch.full(({n},), 3.0, device="cuda"), torch.zeros({n}, device="cuda", dtype=torch.bfloat16)
+row, norm, each, g = torch.zeros({n}, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda"), torch.cuda.CUDAGraph()
+lx, lw = dr.Layout([{n}], dr.F32), dr.Layout.of([w])
+with torch.cuda.graph(g):
+    lx.norm([x], norm, each=each)
+    lx.pack([x], row, max_norm=1.0)
+    lw.update([w], row, 1.0, max_norm=0.5)
+    lx.clip([x], 2.0, out=[row])
+g.replay()
+torch.cuda.synchronize()
+n = {n} ** 0.5
+assert abs(norm.item() - 3 * n) < 1e-6 * n and each.item() == norm.item()
+assert abs(w[7].item() + 0.5 / n) < 0.01 / n and abs(row[5].item() - 2 / n) < 1e-6 / n
+"""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
+
+
+def test_native_and_python_lists_are_the_same(monkeypatch):
+    """The natively listed addresses, those that binding.py lists, and torch's own function in the place of the built one."""
+    dr = _dr()
+    from paper_1803_09877_b200 import binding
+    l = List([1000, 7, 0, 64], ["bf16", "f32", "f16", "f32"], [0, 3], seed=81, absent={3})
+    lay, results = _layout(l), []
+    tensors = [torch.nn.Parameter(l.tensors[0]), l.tensors[1], l.tensors[2], None]
+
+    def run():
+        norm, row, each = torch.zeros(1, device="cuda"), torch.full((1071,), 5.0, device="cuda"), torch.zeros(4, device="cuda")
+        lay.norm(tensors, norm, each=each)
+        lay.pack(tuple(tensors), row, max_norm=0.5)
+        out = List(l.sizes, l.types, [0, 3], like=l, absent={3})
+        lay.clip(tensors, 0.25, out=out.tensors)
+        results.append([norm, row, each] + out.tensors[:3])
+
+    run()
+    own = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+    if own is not None and binding._native is not binding._CtypesCalls:
+        binding._native.set_exchange(torch.Tensor, torch.nn.Parameter, own)
+        run()
+        binding._native.set_exchange(torch.Tensor, torch.nn.Parameter, binding._exchange(torch))
+    monkeypatch.setattr(binding, "_native", binding._CtypesCalls)
+    run()
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert torch.equal(a, b)
+
+
 def test_a_captured_step_on_new_values():
     """Clip, pack and update captured together; replays work on what the tensors then hold, and eager calls go on in between."""
     sizes, types = [30_000, 10, 4097, 1], ["bf16", "f32", "f16", "f32"]
@@ -466,6 +527,51 @@ def test_a_captured_step_on_new_values():
         for x, y in zip(got, [row, master, norms, each] + l.tensors + w.tensors):
             assert torch.equal(x, y)
         assert float(row.norm()) == pytest.approx(0.25, rel=1e-2)
+
+
+@pytest.mark.parametrize("shifts", ["aligned", "all"])
+@pytest.mark.parametrize("types", [["bf16", "f32", "f16", "bf16"], ["f32"] * 4, ["bf16"] * 4])
+def test_long_lists(types, shifts):
+    """Long enough for second passes in several waves of blocks."""
+    sizes = [23_000_001, 17, 12_000_000, 14_000_002]
+    l = List(sizes, types, SHIFTS[shifts], seed=71)
+    lay, d = _layout(l), sum(sizes)
+    parts = [x.double() for x in l.tensors]
+    v = math.sqrt(float(sum(torch.dot(p, p) for p in parts)))
+    norm, row = torch.zeros(1, device="cuda"), torch.full((d + 3,), SENTINEL, device="cuda")
+    off = l.norm_tolerance + U
+
+    def near(got, want, t, off):
+        bound = want.abs() * ((1 + off) * (1 + U) * (1 + HALF_STEP[t]) - 1 if t != "f32" else off + U + off * U) * (1 + 1e-9) + SMALLEST[t] + 2.0 ** -150
+        assert bool(((got.double() - want).abs() <= bound).all())
+
+    lay.pack(l.tensors, row[1:d + 1], max_norm=1.0, norm=norm)
+    _near(norm, v, l.norm_tolerance)
+    near(row[1:d + 1], torch.cat(parts) / v, "f32", off)
+    assert row[0].item() == SENTINEL and bool((row[d + 1:] == SENTINEL).all())
+    out = List(sizes, types, SHIFTS["three"], like=l)
+    lay.clip(l.tensors, 1.0, out=out.tensors)
+    for x, p, t in zip(out.tensors, parts, types):
+        near(x, p / v, t, off)
+    assert out.around_is_untouched()
+    lay.clip(l.tensors, 1.0)
+    for x, p, t in zip(l.tensors, parts, types):
+        near(x, p / v, t, off)
+    assert l.around_is_untouched()
+    u = row[:d].clone()
+    u[0] = 0.0
+    r = float(u.double().square().sum().sqrt())
+    for master in (None, torch.randn(d, device="cuda")):
+        old = [x.double() for x in l.tensors] if master is None else list(master.double().split(sizes))
+        lay.update(l.tensors, u, 2.0, max_norm=0.5, master=master, norm=norm)
+        _near(norm, r, U * (1 + 1e-6))
+        for x, o, step, t in zip(l.tensors, old, u.double().split(sizes), types):
+            step = step * (2.0 * 0.5 / r)
+            fp32 = step.abs() * 3 * U * (1 + 1e-6) + (o - step).abs() * U + 2.0 ** -149
+            assert bool(((x.double() - (o - step)).abs() <= fp32 + ((o - step).abs() + fp32) * HALF_STEP[t] + SMALLEST[t]).all())
+        if master is not None:
+            assert torch.equal(torch.cat([x.float() for x in l.tensors]), torch.cat([m.to(TYPES[t]).float() for m, t in zip(master.split(sizes), types)]))
+    assert l.around_is_untouched()
 
 
 def test_offsets_beyond_32_bits():
