@@ -3,13 +3,17 @@
 //   N = sqrt(sum_t sum_i g_t[i]^2)  or  max_t,i |g_t[i]|        c = max_norm / N if N > max_norm, else 1
 //   clip: g_t <- c g_t       pack: row[off_t + i] = c g_t[i]       update: w_t[i] <- w_t[i] - scale c u[off_t + i],  N = |u|
 //
-// All of them stream the list once or twice and are bound by HBM; short ones by the latency of one or two launches.
+// Long lists are bound by HBM: the list is read for its norm (up to 7.0 TB/s: 2.1 GB of fp32 in 300 us; 465 bf16 tensors, 120 MB, in 23.3 us, 5.2 TB/s)
+// and a second time to be scaled, packed or updated (138 M bf16 packed: 47 + 122 us alone, 180 together, 6.1 TB/s of all that moves).  A pass
+// that knew the factor beforehand would read once; the gradients would have to stay on the chip for that.  Short ones are
+// bound by latency: one launch of one cluster, 2.5 to 5 us.
 //
 // Split.  A list is cut into lines of one word a lane, which begin on word boundaries of the tensor's memory, wherever the tensor
-// begins, and the lines are dealt to the warps of the grid in contiguous ranges of equal length, so that a tensor of any size costs
-// what it holds.  The ranges depend on sizes alone and are made once, with the layout; the tensors' addresses come with every call, as
-// kernel parameters (a graph captures them, nothing is uploaded), at most kMaxPointers a launch; longer lists take several launches.
-// No warp waits for another: block sums are written out and added up, in a fixed order, by whoever needs the norm next.
+// begins, and the lines are dealt to warps in contiguous chunks of equal cost, so that a tensor of any size takes what it holds.
+// The chunks depend on sizes alone and are made once, with the layout; the tensors' addresses come with every call, as kernel
+// parameters (a graph captures them, nothing is uploaded), at most kMaxPointers a launch; longer lists take several launches.
+// No warp waits for one of another block but at a cluster's hardware barrier: block sums are written out and added up, in a fixed
+// order, by whoever needs the norm next.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -30,17 +34,24 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kBlocksPerSm = 4;
 constexpr int kMaxPointers = 2000;                // two lists of 8-byte pointers within the 32,764 bytes of kernel parameters
 constexpr int64_t kMostElements = (int64_t)1 << 40; // a warp counts its lines and their elements in 32 bits
-constexpr int kMinLines = 4;                      // a warp's, before the list gets another one
-constexpr int kVisit = 8;
+constexpr int kBatch = 8;                           // lines that a warp loads at once
+
+// Chunks.  A tensor that a warp comes to costs it as much time as kVisit lines, the wait for its first ones: lists of many small tensors are
+// spread over more warps (norm of 300 bf16 tensors, 300 k elements in all: 10.7 us by lines alone, 4.2 with 8; 465 tensors, 60.2 M,
+// 25.7 and 23.3).  kMinLines: cost of a chunk before the list gets another warp; 2, 4 and 8 within 5 % of one another, 4 ahead.
+constexpr int kVisit = 8, kMinLines = 4;
 // Second passes of long lists: several waves of blocks with short chunks.  SMs that are further from memory take longer over the same share, and
-// with one wave the last of them holds the others up (138 M bf16 packed: one wave 201 us, chunks of 24 lines 185, of 12 182, of 8 181; with a
-// master copy updated, 60.2 M 186, 176, 173, 171).  Below kWaveLines lines a warp one wave is level or faster.
+// with one wave the last of them holds the others up (138 M bf16 packed: one wave 201 us, chunks of 24 lines 185, of 12 182, of 8 180, of 4 208; with
+// a master copy updated, 60.2 M 186, 176, 173, 171, 169).  Below kWaveLines lines a warp one wave is level or faster.  Warps that draw chunks from a
+// counter instead wait for it (253 us).
 constexpr int kWaveLines = 32, kWavesLines = 8, kWaves = 64;
 // In place most calls have nothing to write, and blocks that only find that out cost 1.2 us a thousand: always one wave (1.0e9 bf16 below the limit
 // 296 us, chunks of 64 lines 306, of 8 346; above it 966, 925, 901).
-// A list of up to kSmallTensors tensors and so many lines is left to one cluster of blocks.
+
+// A list of up to kSmallTensors tensors that costs at most kSmallLines lines a warp is left to one cluster of up to kSmallBlocks blocks: one launch
+// instead of two, 4 us of the caller's time instead of 6.5.  GPU time, two launches / one: clip of 2000 fp32 values 6.6 / 3.5 us, of 100,000 in 20 tensors
+// 4.3 / 4.6, of 150,000 4.4 / 5.7.
 constexpr int kSmallTensors = 512, kSmallBlocks = 16, kSmallLines = 8;
-constexpr int kBatch = 8;                         // lines that a warp loads at once
 
 // Lines: 512 bytes of a tensor's own type (one 16-byte word a lane) where the tensor alone is walked, 128 elements (four a lane) where
 // it goes beside its part of a flat vector.
@@ -51,7 +62,7 @@ struct TensorInfo {
     int64_t flat;          // offset in the flat vector
     int64_t lines[2];      // wherever between two boundaries the tensor starts
     int32_t type;
-    int32_t seg_first;     // partial sums of this tensor alone, one for each warp that has lines of it
+    int32_t seg_first;     // partial sums of this tensor alone, one for each chunk that has lines of it
     int32_t seg_count;
     int32_t pad;
 };
@@ -62,8 +73,8 @@ struct Chunk {             // `left` neighbouring lines: upwards from line `at` 
     int32_t left, tensor, type, pad;
 };
 
-// A chunk a warp, all of equal length.  MEASURE: upwards, one wave of blocks, which leave few sums to add up.  The second passes go
-// back, from the end of the list (and of each chunk), whose part is still in L2.
+// A chunk a warp.  MEASURE: upwards, one wave of blocks, which leave few sums to add up.  The second passes go
+// back, from the end of the list (and of each chunk), part of which is still in L2 (15 rows of 1,000,003 clipped: 35.2 us upwards, 31.4).
 enum { MEASURE = 0, IN_PLACE = 1, BYTES = 2, ELEMENTS = 3, TABLES = 4 };
 
 struct Part {              // the tensors of one launch
@@ -142,7 +153,7 @@ struct alignas(N * size_of(TYPE)) Vec {
 // ---- sums of squares and largest magnitudes, in 64-bit slots ----
 
 // Sums are kept in fp64: products of fp32 values are exact there and neither overflow nor vanish.  Squares of a 16-byte word of 16-bit
-// values are added in fp32 first (they have 22 bits at most; eight of them are good to 2^-22) and in fp64 where that sum leaves the
+// values are added in fp32 first (they have 22 bits at most; eight of them are off by 8 * 2^-24 at most) and in fp64 where that sum leaves the
 // range in which fp32 loses nothing that counts: one conversion a word instead of eight.
 struct SumSquares {
     typedef double Slot;
@@ -299,7 +310,8 @@ struct Range {
     int64_t origin;
     int take, begin, end;
     __device__ Range(int64_t numel, int shift, int64_t line, int take_)
-        : origin(line * 32 * VEC - shift), take(take_), begin(origin < 0 ? shift : 0), end((int)max(min(numel - origin, (int64_t)take_ * 32 * VEC), (int64_t)0)) {}   // the last line may lie behind the tensor
+        : origin(line * 32 * VEC - shift), take(take_), begin(origin < 0 ? shift : 0), // the last line may lie behind the tensor
+          end((int)max(min(numel - origin, (int64_t)take_ * 32 * VEC), (int64_t)0)) {}
 
     // batch(at, low, high) for BATCH lines at a time, `at` this lane's place (from origin on) in the first of them: its words u = 0 .. BATCH - 1,
     // at + 32 VEC u, are all the tensor's where low <= u * 32 VEC <= high.
@@ -431,7 +443,8 @@ each_kernel(const TensorInfo* __restrict__ infos, const typename K::Slot* segmen
     }
 }
 
-// The words of what is written; an input that lies otherwise is read element by element, from L1 but for the first of each word.
+// The words of what is written; an input that lies otherwise is read element by element, from L1 but for the first of each word (60 M fp32
+// scaled 117 us, between addresses that differ 122; packed 71 and 73, bf16 54 and 65; updated 105 and 105, bf16 71 and 73).
 template <int TYPE>
 __device__ __forceinline__ void scale_lines(const void* from, void* to, int64_t numel, int64_t line, int take, float c) {
     constexpr int kVec = 16 / size_of(TYPE);
@@ -443,7 +456,7 @@ __device__ __forceinline__ void scale_lines(const void* from, void* to, int64_t 
     T* q = static_cast<T*>(to) + range.origin;
     by_alignment(shift == behind_word<TYPE>(from), [&](auto how) {
         constexpr bool ALIGNED = decltype(how)::value;
-        constexpr int kOnce = ALIGNED ? kBatch : 1;
+        constexpr int kOnce = ALIGNED ? kBatch : kBatch / 2;
         range.template batches<true, kOnce>([&](int at, int low, int high) {
             V x[kOnce];
 #pragma unroll
@@ -507,7 +520,7 @@ __device__ __forceinline__ void pack_lines(const void* base, float* out, int64_t
     float* q = out + range.origin;
     by_alignment(fours_at<TYPE>(base, shift), [&](auto how) {
         constexpr bool ALIGNED = decltype(how)::value;
-        constexpr int kOnce = ALIGNED ? kBatch : 2;
+        constexpr int kOnce = kBatch;
         range.template batches<true, kOnce>([&](int at, int low, int high) {
             Vec<TYPE, kVec> x[kOnce];
 #pragma unroll
@@ -563,7 +576,7 @@ __device__ __forceinline__ void update_lines(void* base, const float* u, float* 
     O* o = MASTER ? reinterpret_cast<O*>(master + flat + range.origin) : reinterpret_cast<O*>(w);
     by_alignment(MASTER ? fours_at<TYPE>(base, shift) : ((flat - shift) & 3) == 0, [&](auto how) {
         constexpr bool ALIGNED = decltype(how)::value;     // the other side: u, or w beside its master copy
-        constexpr int kOnce = ALIGNED ? kBatch / 2 : 1;    // two inputs
+        constexpr int kOnce = kBatch / 2;                  // two inputs
         range.template batches<true, kOnce>([&](int at, int low, int high) {
             Vec<DRACO_F32, kVec> x[kOnce];
             Vec<OLD, kVec> old[kOnce];
@@ -843,6 +856,11 @@ int with_capacity(int count, F f) {
     return f(std::integral_constant<int, kMaxPointers>());
 }
 
+template <class F>
+int with_kind(int kind, F f) {
+    return kind == DRACO_NORM_2 ? f(SumSquares()) : f(MaxMagnitude());
+}
+
 template <int N>
 Pointers<N> pointers_of(const void* const* list, int count) {
     Pointers<N> p;
@@ -868,19 +886,15 @@ int measure(draco_layout* l, const void* const* list, const float* u, int kind, 
         const int rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
             const Pointers<N> p = pointers_of<N>(list ? list + part.first : flat, part.count);
-            auto go = [&](auto kernel, auto* slot) {
-                typedef decltype(slot) S;
+            with_kind(kind, [&](auto what) {
+                typedef decltype(what) K;
+                typedef typename K::Slot* S;
+                const auto kernel = segments ? measure_kernel<K, N, true> : measure_kernel<K, N, false>;
                 launch_dependent(kernel, dim3(part.blocks[MEASURE]), dim3(kThreads), 0, st, p, (const TensorInfo*)l->infos_dev + part.first,
                                  (const Chunk*)l->chunks_dev + part.table[MEASURE], (S)slots, block0, blocks, l->ticket_dev, (S)segs, finish, max_norm, norm,
                                  limit ? l->result_dev : nullptr);
-            };
-            if (kind == DRACO_NORM_2) {
-                if (segments) go(measure_kernel<SumSquares, N, true>, (double*)nullptr);
-                else go(measure_kernel<SumSquares, N, false>, (double*)nullptr);
-            } else {
-                if (segments) go(measure_kernel<MaxMagnitude, N, true>, (unsigned long long*)nullptr);
-                else go(measure_kernel<MaxMagnitude, N, false>, (unsigned long long*)nullptr);
-            }
+                return 0;
+            });
             DRACO_CUDA(cudaGetLastError());
             return DRACO_OK;
         });
@@ -890,13 +904,13 @@ int measure(draco_layout* l, const void* const* list, const float* u, int kind, 
 }
 
 int finish_each(draco_layout* l, int kind, float max_norm, float* norm, float* each, float* factors, cudaStream_t st) {
-    auto go = [&](auto kernel, auto* slot) {
-        typedef const std::remove_pointer_t<decltype(slot)>* S;
-        launch_dependent(kernel, dim3(l->count + 1), dim3(kThreads), 0, st, (const TensorInfo*)l->infos_dev, (S)l->segments_dev, (S)l->slots_dev, l->all_blocks,
-                         max_norm, norm, each, factors);
-    };
-    if (kind == DRACO_NORM_2) go(each_kernel<SumSquares>, (double*)nullptr);
-    else go(each_kernel<MaxMagnitude>, (unsigned long long*)nullptr);
+    with_kind(kind, [&](auto what) {
+        typedef decltype(what) K;
+        typedef const typename K::Slot* S;
+        launch_dependent(each_kernel<K>, dim3(l->count + 1), dim3(kThreads), 0, st, (const TensorInfo*)l->infos_dev, (S)l->segments_dev, (S)l->slots_dev,
+                         l->all_blocks, max_norm, norm, each, factors);
+        return 0;
+    });
     DRACO_CUDA(cudaGetLastError());
     return DRACO_OK;
 }
@@ -933,7 +947,7 @@ int distinct(const draco_layout* l, const void* const* to, const void* const* fr
     struct Entry { uintptr_t address; int tensor; };
     Entry stack[kStack], *table = stack;
     int size = 64;
-    while (size < 4 * l->count) size *= 2;                 // at most half full with both lists
+    while (size < 2 * l->count) size *= 2;                 // at most half full: `from` is only looked up
     if (size > kStack) {
         table = static_cast<Entry*>(malloc(sizeof(Entry) * size));
         if (!table) return DRACO_ENOMEM;
@@ -962,11 +976,6 @@ template <class F>
 int with_small_capacity(int count, F f) {
     if (count <= 64) return f(std::integral_constant<int, 64>());
     return f(std::integral_constant<int, kSmallTensors>());
-}
-
-template <class F>
-int with_kind(int kind, F f) {
-    return kind == DRACO_NORM_2 ? f(SumSquares()) : f(MaxMagnitude());
 }
 
 // launch_dependent with all blocks in one cluster.
@@ -1005,7 +1014,10 @@ cudaError_t allow_large_clusters() {
 bool large_cluster_fits(int count, int blocks) {
     return with_small_capacity(count, [&](auto n) -> int {
         constexpr int N = decltype(n)::value;
-        if (allow_large_clusters<SumSquares, N>() != cudaSuccess || allow_large_clusters<MaxMagnitude, N>() != cudaSuccess) return 0;
+        if (allow_large_clusters<SumSquares, N>() != cudaSuccess || allow_large_clusters<MaxMagnitude, N>() != cudaSuccess) {
+            cudaGetLastError();
+            return 0;
+        }
         cudaLaunchAttribute attr = {};
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = blocks;
