@@ -358,7 +358,8 @@ class Layout:
     """draco_layout: sizes and types of a list of tensors, on the current device.
 
     ``numels``: the numbers of elements.  ``types``: F32, BF16, F16 or torch's dtypes, one for each tensor or one for all.  The calls
-    take the list itself: tensors of these sizes and types on the layout's device, None for one that is absent, or raw addresses.
+    take the list itself (any iterable, ``model.parameters()`` too): tensors of these sizes and types on the layout's device, None for
+    one that is absent, or raw addresses.
     ``norm`` and ``clip`` take tensors that are dense in any order of their dimensions; ``pack`` and ``update``, whose flat vectors
     follow the order of the elements, contiguous ones.
     """
@@ -413,7 +414,16 @@ class Layout:
             raise DracoError(f"{what} is on {x.device}, not on cuda:{self.device}")
         if not (x.is_contiguous() if ordered else _dense(x)):
             raise DracoError(f"{what} is not {'contiguous' if ordered else 'dense'}: strides {x.stride()}")
-        return x.data_ptr()
+        if x.is_neg():
+            raise DracoError(f"{what} is a negated view: its memory holds other values")
+        address = x.data_ptr()
+        if numel and not address:                              # a wrapper without memory of its own, not a tensor that is absent
+            raise DracoError(f"{what} has no memory")
+        return address
+
+    @staticmethod
+    def _sequence(tensors):
+        return tensors if isinstance(tensors, (list, tuple)) else list(tensors)
 
     def _list(self, tensors, what, ordered):
         if len(tensors) != len(self.numels):
@@ -425,6 +435,7 @@ class Layout:
 
     def norm(self, tensors, norm, each=None, kind: int = NORM_2, stream=None):
         """draco_norm: norm <- the norm of all tensors, each[t] <- that of tensor t."""
+        tensors = self._sequence(tensors)
         rc = _native.norm(self._address, self._meta_address, tensors, norm, each, kind, stream)
         if rc is not NotImplemented:
             return rc
@@ -435,6 +446,7 @@ class Layout:
         """draco_clip: the tensors scaled so that their norm (separately: that of each) is at most max_norm, in place or to ``out``.
 
         An ``out`` tensor has the memory order of its input."""
+        tensors, out = self._sequence(tensors), None if out is None else self._sequence(out)
         rc = _native.clip(self._address, self._meta_address, tensors, max_norm, out, norm, each, separately, kind, stream)
         if rc is not NotImplemented:
             return rc
@@ -450,6 +462,7 @@ class Layout:
 
     def pack(self, tensors, row, max_norm: float = float("inf"), norm=None, kind: int = NORM_2, stream=None):
         """draco_pack: the tensors one after the other in the fp32 row, clipped."""
+        tensors = self._sequence(tensors)
         rc = _native.pack(self._address, self._meta_address, tensors, row, max_norm, norm, kind, stream)
         if rc is not NotImplemented:
             return rc
@@ -458,6 +471,7 @@ class Layout:
 
     def update(self, params, u, scale: float, max_norm: float = float("inf"), master=None, norm=None, kind: int = NORM_2, stream=None):
         """draco_update: params <- params - scale * c * u, by way of the fp32 master copy where there is one."""
+        params = self._sequence(params)
         rc = _native.update(self._address, self._meta_address, params, u, scale, max_norm, master, norm, kind, stream)
         if rc is not NotImplemented:
             return rc

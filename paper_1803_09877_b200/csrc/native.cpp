@@ -168,7 +168,7 @@ bool as_told(PyObject* x, int64_t numel, int type, int device, bool ordered, DLT
         return false;
     int64_t n = 1;
     for (int k = 0; k < t->ndim; ++k) n *= t->shape[k];
-    return n == numel && dense(*t, ordered);
+    return n == numel && (t->data || !n) && dense(*t, ordered);
 }
 
 // Address of an fp32 vector of n elements, an int or None.

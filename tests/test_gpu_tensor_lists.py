@@ -377,6 +377,8 @@ def test_refusals():
     refused(lambda: lay.norm([a, c[:20], c], norm), "float16, not 20 of type 1")
     refused(lambda: lay.norm([a.cpu(), b, c], norm), "is on cpu")
     refused(lambda: lay.norm([torch.zeros(20, device="cuda")[::2], b, c], norm), "not dense")
+    refused(lambda: lay.norm([torch.zeros(10, dtype=torch.complex64, device="cuda").conj().imag, b, c], norm), "not dense")
+    refused(lambda: lay.norm([torch._neg_view(a), b, c], norm), "negated")
     refused(lambda: lay.norm([a, b, c], None), "invalid argument")
     refused(lambda: lay.norm([a, b, c], torch.zeros(1, dtype=torch.float64, device="cuda")), "norm")
     refused(lambda: lay.norm([a, b, c], norm, each=torch.zeros(2, device="cuda")), "each")
@@ -415,6 +417,39 @@ def test_refusals():
     assert binding.lib.draco_strerror(binding.ELIMIT).startswith(b"size exceeds")
     lay.close()
     refused(lambda: lay.norm([a, b, c], norm), "invalid argument")
+
+
+def test_some_outputs_in_place():
+    """An output may be its own input, the others elsewhere."""
+    for sizes in ([100, 37, 2000], [400_000, 37, 300_001]):
+        l = List(sizes, ["f32", "bf16", "f16"], [1], seed=91)
+        out = List(sizes, ["f32", "bf16", "f16"], [2], like=l)
+        parts, lay = l.wide(), _layout(l)
+        v = _norm64(parts, "2")
+        targets = [l.tensors[0], out.tensors[1], l.tensors[2]]
+        untouched = out.bits()
+        lay.clip(l.tensors, 0.5, out=targets)
+        for x, p, t in zip(targets, parts, l.types):
+            _scaled_ok(x.double().cpu().numpy(), p, 0.5 / v, t, l.norm_tolerance + U)
+        assert np.array_equal(l.tensors[1].double().cpu().numpy(), parts[1]) and l.around_is_untouched() and out.around_is_untouched()
+        assert torch.equal(out.memory[0][0], untouched[0]) and torch.equal(out.memory[2][0], untouched[2])
+
+
+def test_as_many_tensors_as_there_may_be():
+    dr = _dr()
+    from paper_1803_09877_b200 import binding
+    n = binding.MAX_TENSORS
+    x = torch.ones(n, device="cuda")
+    lay, address = dr.Layout([1] * n, dr.F32), x.data_ptr()
+    addresses = [address + 4 * i for i in range(n)]
+    norm, row = torch.zeros(1, device="cuda"), torch.zeros(n, device="cuda")
+    lay.norm(addresses, norm)
+    assert norm.item() == math.sqrt(n)
+    lay.clip(addresses, math.sqrt(n) / 4)
+    lay.pack(addresses, row)
+    assert bool((row == 0.25).all())
+    lay.update(addresses, row, 2.0)
+    assert bool((x == -0.25).all())
 
 
 def test_two_lists_on_two_streams():
@@ -470,15 +505,18 @@ def test_native_and_python_lists_are_the_same(monkeypatch):
     lay, results = _layout(l), []
     tensors = [torch.nn.Parameter(l.tensors[0]), l.tensors[1], l.tensors[2], None]
 
-    def run():
+    def run(kind=list):
         norm, row, each = torch.zeros(1, device="cuda"), torch.full((1071,), 5.0, device="cuda"), torch.zeros(4, device="cuda")
-        lay.norm(tensors, norm, each=each)
-        lay.pack(tuple(tensors), row, max_norm=0.5)
+        lay.norm(kind(tensors), norm, each=each)
+        lay.pack(kind(tensors), row, max_norm=0.5)
         out = List(l.sizes, l.types, [0, 3], like=l, absent={3})
         lay.clip(tensors, 0.25, out=out.tensors)
         results.append([norm, row, each] + out.tensors[:3])
 
     run()
+    run(tuple)
+    run(iter)
+    run(lambda ts: [None if t is None else t.data_ptr() for t in ts])
     own = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
     if own is not None and binding._native is not binding._CtypesCalls:
         binding._native.set_exchange(torch.Tensor, torch.nn.Parameter, own)
