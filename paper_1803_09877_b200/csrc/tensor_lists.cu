@@ -134,7 +134,10 @@ struct alignas(N * size_of(TYPE)) Vec {
         }
         return x;
     }
-    __device__ float value(int i) const { return Elements<TYPE>::value(element(i)); }
+    __device__ float value(int i) const {
+        if (TYPE == DRACO_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);     // the upper half of an fp32
+        return Elements<TYPE>::value(element(i));
+    }
     __device__ bool any() const {                          // other than zeros of either sign, 16-bit types
         uint32_t bits = 0;
 #pragma unroll
