@@ -19,7 +19,7 @@
  * parameter says "host"); the library never frees or keeps them.  A plan owns
  * its code tables and a small device scratch area allocated by
  * draco_plan_create (kilobytes to a few hundred kilobytes), released by
- * draco_plan_destroy.  Device pointers must be 16-byte aligned.
+ * draco_plan_destroy.  Device pointers must be 16-byte aligned unless a call says otherwise.
  *
  * Streams.  `stream` is a cudaStream_t passed as void* (NULL = the default
  * stream).  Calls enqueue work and return without synchronising unless stated.
@@ -273,11 +273,13 @@ int draco_corrupt(const draco_plan* plan, void* R, const int* adv_idx, const int
  * These calls stand between the two: norms and clipping of a list, a list packed into a row of G for draco_encode, and the decoded
  * sum applied to a list of parameters.  (The paper has no counterpart: its model is one vector.)
  *
- * A layout holds the sizes and types of one list, the split of the work over warps (48 bytes for every 4 KB of a long list, at most 30 MB)
- * and scratch for partial sums (at most 200 KB and 80 bytes a tensor), all in device memory that draco_layout_create allocates.  Tensor t takes entries off_t .. off_t + numel[t] - 1 of the flat vector, off_t = numel[0] + .. + numel[t-1];
+ * A layout holds the sizes and types of one list, the split of the work over warps (48 bytes for every 4 KB of a long list, at most 30 MB
+ * for every 2000 tensors) and scratch for partial sums (at most 200 KB and 100 bytes a tensor), all in device memory that
+ * draco_layout_create allocates.  Tensor t takes entries off_t .. off_t + numel[t] - 1 of the flat vector, off_t = numel[0] + .. + numel[t-1];
  * d = their sum (draco_layout_size).  Each call takes the list as a host array of device addresses, read before the call returns.
  * Tensors are dense (numel contiguous elements); an address needs the alignment of its element only.  NULL: the tensor is absent (a
- * parameter without a gradient).  Sizes of zero are allowed.  The rows of G are such a list too.
+ * parameter without a gradient).  Sizes of zero are allowed.  The rows of G are such a list too.  Tensors that a call writes must not
+ * overlap one another (one address twice is refused; views that overlap in part are the caller's to avoid).
  *
  * Norms: DRACO_NORM_2, sqrt(sum g^2), or DRACO_NORM_MAX, max |g|, over all tensors that are present; sums in fp64, results rounded to fp32.
  * Clipping: factor c = max_norm / norm where norm > max_norm, else 1 (max_norm >= 0; INFINITY: no clipping).  A norm that is not
@@ -291,8 +293,7 @@ enum { DRACO_F32 = 0, DRACO_BF16 = 1, DRACO_F16 = 2 };
 enum { DRACO_NORM_2 = 0, DRACO_NORM_MAX = 1 };
 #define DRACO_MAX_TENSORS 65536
 
-/* numel, type: host arrays of `count` entries.  DRACO_ELIMIT: more than DRACO_MAX_TENSORS tensors or 2^40
- * elements. */
+/* numel, type: host arrays of `count` entries.  DRACO_ELIMIT: more than DRACO_MAX_TENSORS tensors or 2^40 elements. */
 int draco_layout_create(int count, const int64_t* numel /*host*/, const int* type /*host*/, draco_layout** out);
 int draco_layout_destroy(draco_layout* layout);
 int64_t draco_layout_size(const draco_layout* layout);

@@ -1220,7 +1220,8 @@ int draco_clip(draco_layout* layout, const void* const* tensors, void* const* ou
         const Part& part = layout->parts[k];
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
-            launch_dependent(scale_kernel<N>, dim3(part.blocks[table]), dim3(kThreads), 0, st, pointers_of<N>(tensors + part.first, part.count), pointers_of<N>(to + part.first, part.count),
+            launch_dependent(scale_kernel<N>, dim3(part.blocks[table]), dim3(kThreads), 0, st,
+                             pointers_of<N>(tensors + part.first, part.count), pointers_of<N>(to + part.first, part.count),
                              (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[table], limit,
                              separately ? (const float*)layout->factors_dev + part.first : nullptr, !out);
             DRACO_CUDA(cudaGetLastError());
@@ -1260,8 +1261,8 @@ int draco_pack(draco_layout* layout, const void* const* tensors, int kind, float
 }
 
 int draco_update(draco_layout* layout, void* const* params, const float* u, float* master, int kind, float max_norm, float scale, float* norm, void* stream) {
-    if (!layout || !addresses_ok(layout, params) || !kind_ok(kind) || !(max_norm >= 0.0f) || !(scale == scale) || (!u && layout->size) || !aligned16(u) || !aligned16(master) ||
-        !aligned4(norm) || !on_device(layout))
+    if (!layout || !addresses_ok(layout, params) || !kind_ok(kind) || !(max_norm >= 0.0f) || !(scale == scale) || (!u && layout->size) ||
+        !aligned16(u) || !aligned16(master) || !aligned4(norm) || !on_device(layout))
         return DRACO_EINVAL;
     const int64_t bytes = 4 * layout->size;
     const uintptr_t x = reinterpret_cast<uintptr_t>(u), y = reinterpret_cast<uintptr_t>(master);
@@ -1290,7 +1291,8 @@ int draco_update(draco_layout* layout, void* const* params, const float* u, floa
             constexpr int N = decltype(n)::value;
             auto go = [&](auto kernel) {
                 launch_dependent(kernel, dim3(part.blocks[ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(params + part.first, part.count),
-                                 (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[ELEMENTS], u, master, scale, limit);
+                                 (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[ELEMENTS], u, master,
+                                 scale, limit);
             };
             if (master) go(update_kernel<N, true>);
             else go(update_kernel<N, false>);

@@ -69,3 +69,42 @@ def test_dense_tensors():
     assert b._dense(x) and b._dense(x.permute(2, 0, 1)) and b._dense(torch.zeros(2, 3, 4, 5).to(memory_format=torch.channels_last))
     assert b._dense(x[1]) and b._dense(x[:, :1, :1][:1]) and b._dense(torch.zeros(0, 3))
     assert not b._dense(x[:, :, ::2]) and not b._dense(x[:, 1:]) and not b._dense(torch.zeros(3, 1).expand(3, 4)) and not b._dense(x[:, :1, :1])
+
+
+def _native_arguments(call, layout, meta, tensors):
+    return {"norm": (layout, meta, tensors, None, None, 0, 7), "clip": (layout, meta, tensors, 1.0, None, None, None, False, 0, 7),
+            "pack": (layout, meta, tensors, None, 1.0, None, 0, 7), "update": (layout, meta, tensors, None, 1.0, 1.0, None, None, 0, 7)}[call]
+
+
+@pytest.mark.parametrize("call", ["norm", "clip", "pack", "update"])
+def test_native_calls_leave_what_is_unusual_to_python(call):
+    b = _binding()
+    import torch
+    b._find_exchange(torch)
+    meta = b._Meta(2, 9, (ctypes.c_int64 * 2)(4, 5), (ctypes.c_int32 * 2)(b.F32, b.BF16), 0)
+    at, native = ctypes.addressof(meta), getattr(b._native, call)
+    right = [torch.zeros(4), torch.zeros(5, dtype=torch.bfloat16)]             # but on the host
+    for tensors in (right, right[:1], iter(right), [right[1], right[0]], [torch.zeros(4).to_sparse(), None], [object(), None], [4096, None], None):
+        assert native(*_native_arguments(call, None, at, tensors)) is NotImplemented
+        assert getattr(b._CtypesCalls, call)(*_native_arguments(call, None, at, tensors)) is NotImplemented
+    if b._native is not b._CtypesCalls:
+        for tensors in ([None, None], (None, None)):
+            with pytest.raises(b.DracoError, match="invalid argument"):        # no layout, as after close()
+                native(*_native_arguments(call, None, at, tensors))
+        with pytest.raises(TypeError):
+            native(None, at, right)
+        with pytest.raises(TypeError):
+            native(*[x if x != 0 or isinstance(x, bool) else "2-norm" for x in _native_arguments(call, None, at, [None, None])])
+
+
+def test_any_torch_goes_without_its_module(monkeypatch, tmp_path):
+    """Another torch's module is not taken, and one that cannot be loaded is told of; torch's own function takes its place."""
+    b = _binding()
+    import sysconfig
+    import torch
+    own = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+    monkeypatch.setattr(b, "_PKG", str(tmp_path))
+    assert b._exchange(torch) is own
+    (tmp_path / (f"_torch_tensors-{torch.__version__}" + sysconfig.get_config_var("EXT_SUFFIX"))).write_bytes(b"not a module")
+    with pytest.warns(RuntimeWarning, match="torch's own function"):
+        assert b._exchange(torch) is own
