@@ -27,4 +27,7 @@ struct DLPackExchangeAPI {
     void* current_work_stream;
 };
 
+// The capsule's name where torch_tensors.cpp made it, whose function refuses negated views.
+constexpr char kBuiltExchange[] = "draco_torch_tensors";
+
 }  // namespace

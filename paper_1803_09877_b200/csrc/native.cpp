@@ -117,6 +117,8 @@ PyObject* locate_decode(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 // a tensor, or else by torch, 56 ns; the five attributes cost 370.  A list that is not plain tensors of the layout's sizes and types
 // on its device is left to binding.py (NotImplemented), which takes what is unusual and names what is wrong.
 const DLPackExchangeAPI* g_exchange = nullptr;
+bool g_refuses_negated = false;       // torch's own function does not look at the negative bit: its tensors are asked for it
+PyObject* g_is_neg = nullptr;         // "is_neg"
 PyObject *g_tensor = nullptr, *g_parameter = nullptr;       // torch.Tensor and torch.nn.Parameter; their subclasses are left to binding.py
 
 struct Meta {                                               // binding.py's _Meta
@@ -154,13 +156,23 @@ bool dense(const DLTensor& t, bool ordered) {
     return true;
 }
 
+// What the exchange says of a tensor, or false, without an error, where it says nothing or the tensor's memory holds other values than the
+// tensor (a negated view).
+bool tensor_of(PyObject* x, DLTensor* t) {
+    bool plain = g_exchange->tensor_from_object(x, t) == 0;
+    if (plain && !g_refuses_negated) {
+        PyObject* negated = PyObject_CallMethodNoArgs(x, g_is_neg);
+        plain = negated == Py_False;
+        Py_XDECREF(negated);
+    }
+    if (!plain) PyErr_Clear();
+    return plain;
+}
+
 // The tensor as the layout has it, or false, without an error.
 bool as_told(PyObject* x, int64_t numel, int type, int device, bool ordered, DLTensor* t) {
     if (!g_exchange || ((PyObject*)Py_TYPE(x) != g_tensor && (PyObject*)Py_TYPE(x) != g_parameter)) return false;
-    if (g_exchange->tensor_from_object(x, t) != 0) {
-        PyErr_Clear();
-        return false;
-    }
+    if (!tensor_of(x, t)) return false;
     static const DLDataType types[] = {{2, 32, 1}, {4, 16, 1}, {2, 16, 1}};       // DRACO_F32, DRACO_BF16, DRACO_F16
     constexpr int kCuda = 2;
     if (type < 0 || type > 2 || t->device.type != kCuda || t->device.id != device || t->dtype.code != types[type].code ||
@@ -336,9 +348,11 @@ PyObject* set_current_stream(PyObject*, PyObject* args) {     // (raw, device)
 PyObject* set_exchange(PyObject*, PyObject* args) {           // (torch.Tensor, torch.nn.Parameter, its DLPack exchange capsule)
     PyObject *tensor, *parameter, *capsule;
     if (!PyArg_ParseTuple(args, "OOO", &tensor, &parameter, &capsule)) return nullptr;
-    const auto* api = static_cast<const DLPackExchangeAPI*>(PyCapsule_GetPointer(capsule, "dlpack_exchange_api"));
+    const bool built = PyCapsule_IsValid(capsule, kBuiltExchange);
+    const auto* api = static_cast<const DLPackExchangeAPI*>(PyCapsule_GetPointer(capsule, built ? kBuiltExchange : "dlpack_exchange_api"));
     if (!api) return nullptr;
     if (api->major == 1 && api->tensor_from_object) {
+        g_refuses_negated = built;
         keep(g_tensor, tensor);
         keep(g_parameter, parameter);
         g_exchange = api;
@@ -358,5 +372,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nu
 
 PyMODINIT_FUNC PyInit__native(void) {
     g_data_ptr = PyUnicode_InternFromString("data_ptr");
-    return g_data_ptr ? PyModule_Create(&module) : nullptr;
+    g_is_neg = PyUnicode_InternFromString("is_neg");
+    return g_data_ptr && g_is_neg ? PyModule_Create(&module) : nullptr;
 }

@@ -38,7 +38,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_tensors", nullptr, -1, null
 
 PyMODINIT_FUNC PyInit__torch_tensors(void) {
     PyObject* m = PyModule_Create(&module);
-    PyObject* capsule = m ? PyCapsule_New(&api, "dlpack_exchange_api", nullptr) : nullptr;
+    PyObject* capsule = m ? PyCapsule_New(&api, kBuiltExchange, nullptr) : nullptr;
     if (capsule && PyModule_AddObject(m, "exchange", capsule) == 0) return m;
     Py_XDECREF(capsule);
     Py_XDECREF(m);

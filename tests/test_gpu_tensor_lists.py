@@ -681,3 +681,40 @@ def test_an_iteration_from_gradient_tensors_to_weights(code):
     assert np.abs(master.double().cpu().numpy() - want).max() <= err + 0.5 * math.sqrt(d) * err / v * np.abs(exact).max() + 1e-6
     assert torch.equal(torch.cat(weights.tensors), master.bfloat16())
     assert all(l.around_is_untouched() for l in workers) and weights.around_is_untouched()
+
+
+def _exchanges():
+    """The ways to read a list's tensors: the built module, torch's own function, and ctypes, by name; the usual one last."""
+    from paper_1803_09877_b200 import binding
+    native, usual = binding._native, binding._exchange(torch)
+    own = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+
+    def put(calls, exchange):
+        binding._native = calls
+        if calls is not binding._CtypesCalls and exchange is not None:
+            calls.set_exchange(torch.Tensor, torch.nn.Parameter, exchange)
+
+    yield "ctypes", lambda: put(binding._CtypesCalls, None)
+    yield "torch's own", lambda: put(native, own)
+    yield "usual", lambda: put(native, usual)
+
+
+def test_negated_views_are_refused_by_every_exchange():
+    dr = _dr()
+    x, other = torch.ones(4, device="cuda"), torch.zeros(4, device="cuda")
+    negated, part = torch._neg_view(x), torch.ones(1, dtype=torch.complex64, device="cuda").conj().imag
+    lay, one, norm = dr.Layout.of([x]), dr.Layout([1], dr.F32), torch.zeros(1, device="cuda")
+    for name, put in _exchanges():
+        put()
+        try:
+            for l, v in ((lay, negated), (one, part)):
+                row = other[:l.d]
+                for call in (lambda: l.norm([v], norm), lambda: l.clip([v], 0.5), lambda: l.clip([v], 0.5, out=[row]), lambda: l.pack([v], row),
+                             lambda: l.update([v], row, 1.0), lambda: l.pack([row], v), lambda: l.update([row], v, 1.0)):
+                    with pytest.raises(dr.DracoError, match="negated"):
+                        call()
+        finally:
+            for _, back in _exchanges():
+                pass
+            back()
+    assert bool((x == 1.0).all()) and not other.any() and not norm.any()

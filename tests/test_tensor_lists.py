@@ -108,3 +108,71 @@ def test_any_torch_goes_without_its_module(monkeypatch, tmp_path):
     (tmp_path / (f"_torch_tensors-{torch.__version__}" + sysconfig.get_config_var("EXT_SUFFIX"))).write_bytes(b"not a module")
     with pytest.warns(RuntimeWarning, match="torch's own function"):
         assert b._exchange(torch) is own
+
+
+class _DLTensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("device_type", ctypes.c_int32), ("device_id", ctypes.c_int32), ("ndim", ctypes.c_int32),
+                ("code", ctypes.c_uint8), ("bits", ctypes.c_uint8), ("lanes", ctypes.c_uint16), ("shape", ctypes.c_void_p),
+                ("strides", ctypes.c_void_p), ("byte_offset", ctypes.c_uint64)]
+
+
+_READ = ctypes.PYFUNCTYPE(ctypes.c_int, ctypes.py_object, ctypes.POINTER(_DLTensor))
+_capsule_name = ctypes.PYFUNCTYPE(ctypes.c_char_p, ctypes.py_object)(("PyCapsule_GetName", ctypes.pythonapi))
+_capsule_pointer = ctypes.PYFUNCTYPE(ctypes.c_void_p, ctypes.py_object, ctypes.c_char_p)(("PyCapsule_GetPointer", ctypes.pythonapi))
+_new_capsule = ctypes.PYFUNCTYPE(ctypes.py_object, ctypes.c_void_p, ctypes.c_char_p, ctypes.c_void_p)(("PyCapsule_New", ctypes.pythonapi))
+_READERS = (5, 7)                                # places of functions that read a tensor, eight bytes each: DLPack's, and one behind its table
+
+
+def _as_if_on_a_gpu(capsule, keep):
+    """The exchange of this capsule, telling of host tensors as if they were on cuda:0."""
+    name = _capsule_name(capsule)
+    words = 8 if name != b"dlpack_exchange_api" else 7
+    table = (ctypes.c_uint64 * 8)()
+    ctypes.memmove(table, _capsule_pointer(capsule, name), 8 * words)
+    for place in _READERS:
+        if place < words and table[place]:
+            def read(x, out, real=_READ(table[place])):
+                rc = real(x, out)
+                out.contents.device_type, out.contents.device_id = 2, 0
+                return rc
+            keep.append(_READ(read))
+            table[place] = ctypes.cast(keep[-1], ctypes.c_void_p).value
+    keep += [table, name]
+    return _new_capsule(ctypes.addressof(table), name, None)
+
+
+@pytest.fixture(params=["built", "torch's own"])
+def exchange(request):
+    """The binding with one of the two exchanges in place."""
+    b = _binding()
+    import torch
+    if b._native is b._CtypesCalls:
+        pytest.skip("no native calls")
+    b._find_exchange(torch)
+    own, usual, keep = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None), b._exchange(torch), []
+    chosen = own if request.param == "torch's own" else usual
+    if chosen is None or (request.param == "built" and usual is own):
+        pytest.skip("not there")
+    b._native.set_exchange(torch.Tensor, torch.nn.Parameter, _as_if_on_a_gpu(chosen, keep))
+    yield b
+    b._native.set_exchange(torch.Tensor, torch.nn.Parameter, usual)
+
+
+@pytest.mark.parametrize("call", ["norm", "clip", "pack", "update"])
+def test_negated_views_are_left_to_python(exchange, call):
+    """Their memory holds the other sign, whoever tells of it."""
+    b = exchange
+    import torch
+    meta = b._Meta(1, 4, (ctypes.c_int64 * 1)(4), (ctypes.c_int32 * 1)(b.F32), 0)
+    at, x = ctypes.addressof(meta), torch.ones(4)
+    one = b._Meta(1, 1, (ctypes.c_int64 * 1)(1), (ctypes.c_int32 * 1)(b.F32), 0)
+    with pytest.raises(b.DracoError, match="invalid argument"):                # taken: no layout
+        getattr(b._native, call)(*_native_arguments(call, None, at, [x]))
+    assert getattr(b._native, call)(*_native_arguments(call, None, at, [torch._neg_view(x)])) is NotImplemented
+    part = torch.ones(1, dtype=torch.complex64).conj().imag
+    assert part.is_neg()
+    assert getattr(b._native, call)(*_native_arguments(call, None, ctypes.addressof(one), [part])) is NotImplemented
+    for place, numel in {"norm": [(4, 1)], "clip": [(6, 1)], "pack": [(3, 4)], "update": [(3, 4), (6, 4)]}[call]:        # each, each, row, u and master
+        args = list(_native_arguments(call, None, at, [x]))
+        args[place] = torch._neg_view(torch.ones(numel))
+        assert getattr(b._native, call)(*args) is NotImplemented
