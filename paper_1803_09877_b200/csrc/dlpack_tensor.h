@@ -27,7 +27,12 @@ struct DLPackExchangeAPI {
     void* current_work_stream;
 };
 
-// The capsule's name where torch_tensors.cpp made it, whose function refuses negated views.
+// What torch_tensors.cpp offers, in a capsule of this name: both functions refuse negated views, the second gives the address of memory that
+// may be written.
+struct BuiltExchange {
+    DLPackExchangeAPI read;
+    int (*written_from_object)(void* object, DLTensor* out);
+};
 constexpr char kBuiltExchange[] = "draco_torch_tensors";
 
 }  // namespace

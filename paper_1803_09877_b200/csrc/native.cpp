@@ -117,7 +117,7 @@ PyObject* locate_decode(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 // a tensor, or else by torch, 56 ns; the five attributes cost 370.  A list that is not plain tensors of the layout's sizes and types
 // on its device is left to binding.py (NotImplemented), which takes what is unusual and names what is wrong.
 const DLPackExchangeAPI* g_exchange = nullptr;
-bool g_refuses_negated = false;       // torch's own function does not look at the negative bit: its tensors are asked for it
+const BuiltExchange* g_built = nullptr;                     // the same, if torch_tensors.cpp made it
 PyObject* g_is_neg = nullptr;         // "is_neg"
 PyObject *g_tensor = nullptr, *g_parameter = nullptr;       // torch.Tensor and torch.nn.Parameter; their subclasses are left to binding.py
 
@@ -157,10 +157,11 @@ bool dense(const DLTensor& t, bool ordered) {
 }
 
 // What the exchange says of a tensor, or false, without an error, where it says nothing or the tensor's memory holds other values than the
-// tensor (a negated view).
-bool tensor_of(PyObject* x, DLTensor* t) {
-    bool plain = g_exchange->tensor_from_object(x, t) == 0;
-    if (plain && !g_refuses_negated) {
+// tensor (a negated view; torch's own function does not look at that: the tensor itself is asked).  written: the memory is the tensor's alone;
+// one that shares it until either is written (a lazy clone) gets its own here, from torch's own function in any case.
+bool tensor_of(PyObject* x, bool written, DLTensor* t) {
+    bool plain = (g_built && written ? g_built->written_from_object : g_exchange->tensor_from_object)(x, t) == 0;
+    if (plain && !g_built) {
         PyObject* negated = PyObject_CallMethodNoArgs(x, g_is_neg);
         plain = negated == Py_False;
         Py_XDECREF(negated);
@@ -170,9 +171,9 @@ bool tensor_of(PyObject* x, DLTensor* t) {
 }
 
 // The tensor as the layout has it, or false, without an error.
-bool as_told(PyObject* x, int64_t numel, int type, int device, bool ordered, DLTensor* t) {
+bool as_told(PyObject* x, int64_t numel, int type, int device, bool ordered, bool written, DLTensor* t) {
     if (!g_exchange || ((PyObject*)Py_TYPE(x) != g_tensor && (PyObject*)Py_TYPE(x) != g_parameter)) return false;
-    if (!tensor_of(x, t)) return false;
+    if (!tensor_of(x, written, t)) return false;
     static const DLDataType types[] = {{2, 32, 1}, {4, 16, 1}, {2, 16, 1}};       // DRACO_F32, DRACO_BF16, DRACO_F16
     constexpr int kCuda = 2;
     if (type < 0 || type > 2 || t->device.type != kCuda || t->device.id != device || t->dtype.code != types[type].code ||
@@ -184,10 +185,10 @@ bool as_told(PyObject* x, int64_t numel, int type, int device, bool ordered, DLT
 }
 
 // Address of an fp32 vector of n elements, an int or None.
-bool vector_address(PyObject* x, const Meta* m, int64_t n, void** out) {
+bool vector_address(PyObject* x, const Meta* m, int64_t n, bool written, void** out) {
     if (x == Py_None || PyLong_Check(x)) return address(x, out);
     DLTensor t;
-    if (!as_told(x, n, DRACO_F32, m->device, true, &t)) return false;
+    if (!as_told(x, n, DRACO_F32, m->device, true, written, &t)) return false;
     *out = static_cast<char*>(t.data) + t.byte_offset;
     return true;
 }
@@ -199,7 +200,7 @@ struct Addresses {
         if (p != few) PyMem_Free(p);
     }
     // beside: a list whose tensors have the same sizes and strides
-    bool take(PyObject* list, const Meta* m, bool ordered, PyObject* beside = nullptr) {
+    bool take(PyObject* list, const Meta* m, bool ordered, bool written, PyObject* beside = nullptr) {
         if (!PyList_Check(list) && !PyTuple_Check(list)) return false;
         if (PySequence_Fast_GET_SIZE(list) != m->count) return false;
         if (m->count > (int64_t)(sizeof(few) / sizeof(few[0]))) {
@@ -215,7 +216,7 @@ struct Addresses {
             p[i] = nullptr;
             if (x == Py_None) continue;
             DLTensor t, b;
-            if (!as_told(x, m->numels[i], m->types[i], m->device, ordered, &t)) return false;
+            if (!as_told(x, m->numels[i], m->types[i], m->device, ordered, written, &t)) return false;
             if (beside) {
                 PyObject* y = PySequence_Fast_ITEMS(beside)[i];
                 if (y == Py_None || g_exchange->tensor_from_object(y, &b) != 0) {
@@ -266,7 +267,8 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!layout_of(args, nargs, 7, &layout, &meta)) return nullptr;
     META;
     Addresses a;
-    if (!a.take(args[2], m, false) || !vector_address(args[3], m, 1, &norm) || !vector_address(args[4], m, m->count, &each)) return left_to_python();
+    if (!a.take(args[2], m, false, false) || !vector_address(args[3], m, 1, true, &norm) || !vector_address(args[4], m, m->count, true, &each))
+        return left_to_python();
     if (!whole(args[5], &kind) || !stream_of(args[6], &st)) return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS rc = draco_norm(LAYOUT, a.p, kind, (float*)norm, (float*)each, st);
@@ -282,8 +284,8 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     META;
     Addresses a, b;
     const bool out = args[4] != Py_None;
-    if (!a.take(args[2], m, false) || (out && !b.take(args[4], m, false, args[2])) || !vector_address(args[5], m, 1, &norm) ||
-        !vector_address(args[6], m, m->count, &each))
+    if (!a.take(args[2], m, false, !out) || (out && !b.take(args[4], m, false, true, args[2])) || !vector_address(args[5], m, 1, true, &norm) ||
+        !vector_address(args[6], m, m->count, true, &each))
         return left_to_python();
     const int separately = PyObject_IsTrue(args[7]);
     if (separately < 0 || !number(args[3], &max_norm) || !whole(args[8], &kind) || !stream_of(args[9], &st)) return nullptr;
@@ -300,7 +302,8 @@ PyObject* pack(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!layout_of(args, nargs, 8, &layout, &meta)) return nullptr;
     META;
     Addresses a;
-    if (!a.take(args[2], m, true) || !vector_address(args[3], m, m->d, &row) || !vector_address(args[5], m, 1, &norm)) return left_to_python();
+    if (!a.take(args[2], m, true, false) || !vector_address(args[3], m, m->d, true, &row) || !vector_address(args[5], m, 1, true, &norm))
+        return left_to_python();
     if (!number(args[4], &max_norm) || !whole(args[6], &kind) || !stream_of(args[7], &st)) return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS rc = draco_pack(LAYOUT, a.p, kind, max_norm, (float*)row, (float*)norm, st);
@@ -315,8 +318,8 @@ PyObject* update(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!layout_of(args, nargs, 10, &layout, &meta)) return nullptr;
     META;
     Addresses a;
-    if (!a.take(args[2], m, true) || !vector_address(args[3], m, m->d, &u) || !vector_address(args[6], m, m->d, &master) ||
-        !vector_address(args[7], m, 1, &norm))
+    if (!a.take(args[2], m, true, true) || !vector_address(args[3], m, m->d, false, &u) || !vector_address(args[6], m, m->d, true, &master) ||
+        !vector_address(args[7], m, 1, true, &norm))
         return left_to_python();
     if (!number(args[4], &scale) || !number(args[5], &max_norm) || !whole(args[8], &kind) || !stream_of(args[9], &st)) return nullptr;
     int rc;
@@ -348,11 +351,12 @@ PyObject* set_current_stream(PyObject*, PyObject* args) {     // (raw, device)
 PyObject* set_exchange(PyObject*, PyObject* args) {           // (torch.Tensor, torch.nn.Parameter, its DLPack exchange capsule)
     PyObject *tensor, *parameter, *capsule;
     if (!PyArg_ParseTuple(args, "OOO", &tensor, &parameter, &capsule)) return nullptr;
-    const bool built = PyCapsule_IsValid(capsule, kBuiltExchange);
-    const auto* api = static_cast<const DLPackExchangeAPI*>(PyCapsule_GetPointer(capsule, built ? kBuiltExchange : "dlpack_exchange_api"));
+    const BuiltExchange* built = nullptr;
+    if (PyCapsule_IsValid(capsule, kBuiltExchange)) built = static_cast<const BuiltExchange*>(PyCapsule_GetPointer(capsule, kBuiltExchange));
+    const auto* api = built ? &built->read : static_cast<const DLPackExchangeAPI*>(PyCapsule_GetPointer(capsule, "dlpack_exchange_api"));
     if (!api) return nullptr;
     if (api->major == 1 && api->tensor_from_object) {
-        g_refuses_negated = built;
+        g_built = built;
         keep(g_tensor, tensor);
         keep(g_parameter, parameter);
         g_exchange = api;

@@ -7,6 +7,7 @@
 
 namespace {
 
+template <bool WRITTEN>
 int tensor_from_object(void* object, DLTensor* out) {
     try {
         const at::Tensor& t = THPVariable_Unpack(static_cast<PyObject*>(object));
@@ -19,7 +20,8 @@ int tensor_from_object(void* object, DLTensor* out) {
             case at::kHalf: out->dtype = {2, 16, 1}; break;
             default: return -1;
         }
-        out->data = const_cast<void*>(t.const_data_ptr());
+        // a lazy clone gets memory of its own before it is written
+        out->data = WRITTEN ? t.mutable_data_ptr() : const_cast<void*>(t.const_data_ptr());
         out->byte_offset = 0;
         out->ndim = (int32_t)t.dim();
         out->shape = const_cast<int64_t*>(t.sizes().data());
@@ -30,7 +32,7 @@ int tensor_from_object(void* object, DLTensor* out) {
     }
 }
 
-DLPackExchangeAPI api = {1, 3, nullptr, nullptr, nullptr, nullptr, tensor_from_object, nullptr};
+BuiltExchange api = {{1, 3, nullptr, nullptr, nullptr, nullptr, tensor_from_object<false>, nullptr}, tensor_from_object<true>};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_tensors", nullptr, -1, nullptr, nullptr, nullptr, nullptr, nullptr};
 

@@ -718,3 +718,28 @@ def test_negated_views_are_refused_by_every_exchange():
                 pass
             back()
     assert bool((x == 1.0).all()) and not other.any() and not norm.any()
+
+
+def test_writes_to_a_lazy_clone_leave_its_source():
+    dr = _dr()
+    for name, put in _exchanges():
+        put()
+        try:
+            for write in ("clip", "out", "row", "param", "master"):
+                x, y = torch.full((1000,), 3.0, device="cuda"), torch.full((1000,), 3.0, device="cuda")
+                clone, lay = torch._lazy_clone(x), dr.Layout.of([x])
+                if write == "clip":
+                    lay.clip([clone], 1.0)
+                elif write == "out":
+                    lay.clip([y], 1.0, out=[clone])
+                elif write == "row":
+                    lay.pack([y], clone, max_norm=1.0)
+                elif write == "param":
+                    lay.update([clone], y, 0.5)
+                else:
+                    lay.update([y.clone()], y, 0.5, master=clone)
+                assert bool((x == 3.0).all()) and bool((y == 3.0).all()) and not bool((clone == 3.0).any()), (name, write)
+        finally:
+            for _, back in _exchanges():
+                pass
+            back()

@@ -176,3 +176,34 @@ def test_negated_views_are_left_to_python(exchange, call):
         args = list(_native_arguments(call, None, at, [x]))
         args[place] = torch._neg_view(torch.ones(numel))
         assert getattr(b._native, call)(*args) is NotImplemented
+
+
+@pytest.mark.parametrize("call", ["norm", "clip", "clip to out", "pack", "update"])
+def test_lazy_clones_get_memory_of_their_own_before_they_are_written(exchange, call):
+    """And whose memory else a call writes would be the source's, too."""
+    b = exchange
+    import torch
+    meta = b._Meta(1, 4, (ctypes.c_int64 * 1)(4), (ctypes.c_int32 * 1)(b.F32), 0)
+    name, at = call.split()[0], ctypes.addressof(meta)
+    sources = [torch.ones(4), torch.ones(1), torch.ones(4)]
+    x, scalar, vector = (torch._lazy_clone(t) for t in sources)
+    args = list(_native_arguments(name, None, at, [x]))
+    written = [scalar]
+    if call == "norm":
+        args[3] = scalar
+    elif call == "clip":
+        args[5] = scalar
+        written += [x]
+    elif call == "clip to out":
+        args[4], args[5] = [vector], scalar
+        written += [vector]
+    elif call == "pack":
+        args[3], args[5] = vector, scalar
+        written += [vector]
+    else:
+        args[6], args[7] = vector, scalar
+        written += [x, vector]
+    with pytest.raises(b.DracoError, match="invalid argument"):                # taken: no layout
+        getattr(b._native, name)(*args)
+    assert not any(torch._C._is_cow_tensor(t) for t in written)
+    assert all(bool((t == 1.0).all()) for t in [x, scalar, vector] + sources)
