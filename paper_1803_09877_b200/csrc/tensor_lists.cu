@@ -166,6 +166,7 @@ struct alignas(N * size_of(TYPE)) Vec {
 // range in which fp32 loses nothing that counts: one conversion a word instead of eight.
 struct SumSquares {
     typedef double Slot;
+    static constexpr bool kOrdered = true;                 // roundings depend on the order
     static __device__ Slot zero() { return 0.0; }
     static __device__ void add(Slot& a, Slot b) { a += b; }
     template <int TYPE>
@@ -199,6 +200,7 @@ struct SumSquares {
 // Magnitudes compare like their bit patterns, infinity above all numbers and NaN above infinity; 16-bit ones two at a time.
 struct MaxMagnitude {
     typedef unsigned long long Slot;
+    static constexpr bool kOrdered = false;
     static __device__ Slot zero() { return 0; }
     static __device__ void add(Slot& a, Slot b) { a = a > b ? a : b; }
     template <int TYPE>
@@ -374,26 +376,63 @@ __device__ __forceinline__ void store(typename Elements<TYPE>::type* p, const Ve
     }
 }
 
-template <class K, int TYPE>
-__device__ __forceinline__ void measure_lines(const void* base, int64_t numel, int64_t line, int take, typename K::Slot& acc) {
+// A word as it is loaded: at once (BY = 16), in halves or quarters where it begins on such a boundary, or (2) its first element, three pairs
+// of elements, and the last.
+template <int TYPE, int N, int BY>
+struct Loaded {
+    uint32_t w[BY == 2 ? 5 : 4];
+    __device__ __forceinline__ void load(bool here, const typename Elements<TYPE>::type* p) {
+#pragma unroll
+        for (int i = 0; i < (BY == 2 ? 5 : 4); ++i) w[i] = 0;
+        if (!here) return;
+        if (BY == 16) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else if (BY == 8) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint2 v = reinterpret_cast<const uint2*>(p)[i];
+                w[2 * i] = v.x, w[2 * i + 1] = v.y;
+            }
+        } else if (BY == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+        } else {
+            w[0] = reinterpret_cast<const uint16_t*>(p)[0];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) w[i + 1] = *reinterpret_cast<const uint32_t*>(p + 1 + 2 * i);
+            w[BY == 2 ? 4 : 0] = reinterpret_cast<const uint16_t*>(p)[N - 1];
+        }
+    }
+    __device__ __forceinline__ Vec<TYPE, N> word() const {
+        Vec<TYPE, N> v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.w[i] = BY != 2 ? w[i] : __funnelshift_l(i ? w[i] : w[0] << 16, w[BY == 2 ? i + 1 : i], 16);
+        return v;
+    }
+};
+
+// BY = 16: lines begin on a word's boundary, others on the tensor's first element.
+template <class K, int TYPE, int BY>
+__device__ __forceinline__ void measure_by(const void* base, int shift, int64_t numel, int64_t line, int take, typename K::Slot& acc) {
     constexpr int kVec = 16 / size_of(TYPE);
     typedef typename Elements<TYPE>::type T;
-    typedef Vec<TYPE, kVec> V;
-    const Range<kVec> range(numel, behind_word<TYPE>(base), line, take);
+    typedef Loaded<TYPE, kVec, BY> V;
+    const Range<kVec> range(numel, BY == 16 ? shift : 0, line, take);
     const T* p = static_cast<const T*>(base) + range.origin;
     // One half of a batch comes while the other is added up.  us, eight lines then their sums / halves of four / of two: 60.2 M bf16 23.3, 22.4, 24.7;
-    // 45 rows of 11.7 M fp32 304, 314, 301 (three: 309).
-    constexpr int kHalf = TYPE == DRACO_F32 ? 2 : 4, kStep = kHalf * 32 * kVec;
+    // 45 rows of 11.7 M fp32 304, 314, 301 (three: 309).  Words loaded in pieces: 1 M bf16 in 60 tensors, halves of two, three, four 4.6, 4.8, 5.1.
+    constexpr int kHalf = TYPE == DRACO_F32 || BY < 16 ? 2 : 4, kStep = kHalf * 32 * kVec;
     const int lane = (threadIdx.x & 31) * kVec;
     V x[kHalf], y[kHalf];
     auto fetch = [&](V* v, int at) {
         const int low = range.begin - at, high = range.end - kVec - at;
 #pragma unroll
-        for (int u = 0; u < kHalf; ++u) v[u] = load<TYPE, kVec, true>(DRACO_WHOLE(u), p + at + u * 32 * kVec);
+        for (int u = 0; u < kHalf; ++u) v[u].load(DRACO_WHOLE(u), p + at + u * 32 * kVec);
     };
     auto add = [&](const V* v) {
 #pragma unroll
-        for (int u = 0; u < kHalf; ++u) K::template word<TYPE, kVec>(acc, v[u]);
+        for (int u = 0; u < kHalf; ++u) K::template word<TYPE, kVec>(acc, v[u].word());
     };
     fetch(x, lane);
     for (int i = 0; i < take; i += 2 * kHalf) {
@@ -404,6 +443,20 @@ __device__ __forceinline__ void measure_lines(const void* base, int64_t numel, i
         add(y);
     }
     range.ends([&](int i) { K::template one<TYPE>(acc, p[i]); });
+}
+
+// Where roundings depend on the order of a sum, that order does not depend on the address: the words that are added up begin with the tensor's first
+// element, so that equal gradients have equal norms, to the last bit, and make equal rows.  A tensor that begins elsewhere than on a
+// word's boundary has its words loaded in pieces, at most five, out of L1 but for the first (us, on the boundary and off it: 60.2 M bf16 in 465 tensors
+// 23.4, 29; 45 rows of 11.7 M fp32 302, by halves 305, by quarters 360.  Words joined from two aligned ones, the other by a shuffle: 23.4, 27;
+// 302, 318, but 1 to 2 us for what the two ends of each tensor then need).
+template <class K, int TYPE>
+__device__ __forceinline__ void measure_lines(const void* base, int64_t numel, int64_t line, int take, typename K::Slot& acc) {
+    const int shift = behind_word<TYPE>(base);
+    if (!K::kOrdered || shift == 0) measure_by<K, TYPE, 16>(base, shift, numel, line, take, acc);
+    else if (shift * size_of(TYPE) % 8 == 0) measure_by<K, TYPE, 8>(base, shift, numel, line, take, acc);
+    else if (TYPE == DRACO_F32 || shift % 2 == 0) measure_by<K, TYPE, 4>(base, shift, numel, line, take, acc);
+    else measure_by<K, TYPE, 2>(base, shift, numel, line, take, acc);
 }
 
 // Block sums to slots[blockIdx.x]; finish: the norm of all, too, from the block that finishes last.  SEGMENTS: the sums of each warp's part of each

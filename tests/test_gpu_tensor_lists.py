@@ -743,3 +743,55 @@ def test_writes_to_a_lazy_clone_leave_its_source():
             for _, back in _exchanges():
                 pass
             back()
+
+
+@pytest.mark.parametrize("kind", ["2", "max"])
+@pytest.mark.parametrize("types", [["bf16"], ["f16"], ["f32"], ["bf16", "f32", "f16"]])
+@pytest.mark.parametrize("sizes", [[1], [7], [8], [9], [15], [16], [17], [100], [257], [1000, 33, 511], [2047, 2048, 2049], [4096, 4097, 12_345], [100_003, 5],
+                                   [37 * (i % 9) + i for i in range(120)], [400_003, 1, 70_001], [257 + 64 * (i % 3) for i in range(600)], [3_000_017, 999]])
+def test_results_do_not_depend_on_where_the_tensors_lie(sizes, types, kind):
+    """The same values at other offsets from the 16-byte grid: the same bits, so that equal gradients make equal rows, whoever packs them."""
+    types = (types * len(sizes))[:len(sizes)]
+    l = List(sizes, types, [0], seed=92, sigma=1.0)
+    lay, d = _layout(l), sum(sizes)
+    limit = 0.37 * _norm64(l.wide(), kind)
+    want = None
+    for shifts in ([0], [1], [2], [3], [4], [5], [6], [7], [0, 1, 2, 3, 4, 5, 6, 7], [7, 4, 2]):
+        at = List(sizes, types, shifts, like=l)
+        for x, y in zip(at.tensors, l.tensors):
+            x.copy_(y)
+        norms, each = torch.zeros(3, 1, device="cuda"), torch.zeros(2, len(sizes), device="cuda")
+        row = torch.zeros(d + 3, device="cuda")[shifts[0] % 4:][:d]
+        lay.norm(at.tensors, norms[0], kind=_kind(kind))
+        lay.norm(at.tensors, norms[1], each=each[0], kind=_kind(kind))
+        lay.pack(at.tensors, row, max_norm=limit, norm=norms[2], kind=_kind(kind))
+        got = [norms, each, row]
+        for separately in (False, True):
+            out = List(sizes, types, shifts[::-1], like=l)
+            lay.clip(at.tensors, limit / (2 if separately else 1), out=out.tensors, separately=separately, kind=_kind(kind))
+            got += out.tensors
+        lay.clip(at.tensors, limit, each=each[1], separately=True, kind=_kind(kind))
+        got = [x.clone() for x in got + at.tensors]
+        want = want or got
+        for x, y in zip(got, want):
+            assert torch.equal(x, y), shifts
+
+
+def test_replicas_of_a_group_that_pack_their_own_copies_agree():
+    """The repetition code's vote compares bits: honest members whose gradients lie elsewhere in memory are no disagreement."""
+    dr = _dr()
+    n, s, sizes, types = 9, 1, [700, 31, 1000, 257], ["bf16", "f16", "bf16", "f32"]
+    d = sum(sizes)
+    plan, lay = dr.Plan(n, s, d, dr.REP), dr.Layout(sizes, [TYPES[t] for t in types])
+    flags, u = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(d, device="cuda")
+    for seed in range(40):
+        l = List(sizes, types, [0], seed=200 + seed, sigma=1.0)
+        R = torch.empty((n, d), device="cuda")
+        for k in range(n):
+            mine = List(sizes, types, [k % 8, 3, (2 * k + 1) % 8], like=l)
+            for x, y in zip(mine.tensors, l.tensors):
+                x.copy_(y)
+            lay.pack(mine.tensors, R[k], max_norm=1.0)
+        assert all(torch.equal(R[0], R[k]) for k in range(n))
+        plan.locate_decode(R, None, flags, u)
+        assert not flags.any() and plan.info()["no_majority"] == 0
