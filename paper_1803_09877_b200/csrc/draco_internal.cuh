@@ -113,7 +113,7 @@ int cuda_fail(cudaError_t err, const char* what);
 // kernel writes.  Saves the launch gap, 1 - 2 us a kernel: n = 45, s = 5, d = 4096, locate and decode (three kernels) 37.8 -> 31.8
 // us; n = 15, s = 2, d = 1 M 68.7 -> 63.5 us; a repetition encode of 100,000 coordinates costs the caller 3.8 instead of 4.4 us.
 template <typename... Params, typename... Args>
-void launch_dependent(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+cudaError_t launch_dependent(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
@@ -124,7 +124,7 @@ void launch_dependent(void (*kernel)(Params...), dim3 grid, dim3 block, size_t s
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);    // an error is left for cudaGetLastError, as by <<< >>>
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);    // an error is left for cudaGetLastError, too, as by <<< >>>
 }
 #ifdef __CUDACC__
 __device__ __forceinline__ void pdl_begin() {

@@ -459,7 +459,8 @@ __device__ __forceinline__ void measure_lines(const void* base, int64_t numel, i
     else measure_by<K, TYPE, 2>(base, shift, numel, line, take, acc);
 }
 
-// Block sums to slots[blockIdx.x]; finish: the norm of all, too, from the block that finishes last.  SEGMENTS: the sums of each warp's part of each
+// Block sums to slots[block0 + blockIdx.x]; finish: the norm of all, too, from the block that finishes last (earlier launches of the measurement have
+// finished before this one begins, and one launch either runs or does not, so that the ticket is back at zero whatever happens).  SEGMENTS: the sums of each warp's part of each
 // tensor to segments[warp + tensor], a place of its own for every such pair, since both only grow along the list.
 template <class K, int N, bool SEGMENTS>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
@@ -488,7 +489,7 @@ measure_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __res
         slots[block0 + blockIdx.x] = acc;
         if (finish) {
             __threadfence();
-            last = atomicInc(ticket, all_blocks - 1) == all_blocks - 1; // back at zero after the last
+            last = atomicInc(ticket, gridDim.x - 1) == gridDim.x - 1;  // back at zero after the last
             __threadfence();
         }
     }
@@ -955,7 +956,8 @@ int measure(draco_layout* l, const void* const* list, const float* u, int kind, 
     const int blocks = list ? l->all_blocks : l->parts[l->num_parts].blocks[MEASURE];
     const bool finish = (!limit || later_blocks > one_wave(l)) && !segments;
     if (limit) *limit = {finish ? l->result_dev : nullptr, static_cast<char*>(l->slots_dev) + (list ? 0 : (size_t)l->all_blocks * 8), blocks, kind, max_norm, norm};
-    for (int k = 0; k < (list ? l->num_parts : 1); ++k) {
+    const int launches = list ? l->num_parts : 1;
+    for (int k = 0; k < launches; ++k) {
         const Part& part = l->parts[list ? k : l->num_parts];
         const int block0 = list ? part.block0 : 0;
         char* slots = static_cast<char*>(l->slots_dev) + (list ? 0 : (size_t)l->all_blocks * 8);
@@ -963,17 +965,15 @@ int measure(draco_layout* l, const void* const* list, const float* u, int kind, 
         const int rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
             const Pointers<N> p = pointers_of<N>(list ? list + part.first : flat, part.count);
-            with_kind(kind, [&](auto what) {
+            return with_kind(kind, [&](auto what) -> int {
                 typedef decltype(what) K;
                 typedef typename K::Slot* S;
                 const auto kernel = segments ? measure_kernel<K, N, true> : measure_kernel<K, N, false>;
-                launch_dependent(kernel, dim3(part.blocks[MEASURE]), dim3(kThreads), 0, st, p, (const TensorInfo*)l->infos_dev + part.first,
-                                 (const Chunk*)l->chunks_dev + part.table[MEASURE], (S)slots, block0, blocks, l->ticket_dev, (S)segs, finish, max_norm, norm,
-                                 limit ? l->result_dev : nullptr);
-                return 0;
+                DRACO_CUDA(launch_dependent(kernel, dim3(part.blocks[MEASURE]), dim3(kThreads), 0, st, p, (const TensorInfo*)l->infos_dev + part.first,
+                                            (const Chunk*)l->chunks_dev + part.table[MEASURE], (S)slots, block0, blocks, l->ticket_dev, (S)segs,
+                                            finish && k == launches - 1, max_norm, norm, limit ? l->result_dev : nullptr));
+                return DRACO_OK;
             });
-            DRACO_CUDA(cudaGetLastError());
-            return DRACO_OK;
         });
         if (rc != DRACO_OK) return rc;
     }
@@ -981,15 +981,13 @@ int measure(draco_layout* l, const void* const* list, const float* u, int kind, 
 }
 
 int finish_each(draco_layout* l, int kind, float max_norm, float* norm, float* each, float* factors, cudaStream_t st) {
-    with_kind(kind, [&](auto what) {
+    return with_kind(kind, [&](auto what) -> int {
         typedef decltype(what) K;
         typedef const typename K::Slot* S;
-        launch_dependent(each_kernel<K>, dim3(l->count + 1), dim3(kThreads), 0, st, (const TensorInfo*)l->infos_dev, (S)l->segments_dev, (S)l->slots_dev,
-                         l->all_blocks, max_norm, norm, each, factors);
-        return 0;
+        DRACO_CUDA(launch_dependent(each_kernel<K>, dim3(l->count + 1), dim3(kThreads), 0, st, (const TensorInfo*)l->infos_dev, (S)l->segments_dev,
+                                    (S)l->slots_dev, l->all_blocks, max_norm, norm, each, factors));
+        return DRACO_OK;
     });
-    DRACO_CUDA(cudaGetLastError());
-    return DRACO_OK;
 }
 
 bool on_device(const draco_layout* l) {
@@ -1273,11 +1271,10 @@ int draco_clip(draco_layout* layout, const void* const* tensors, void* const* ou
         const Part& part = layout->parts[k];
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
-            launch_dependent(scale_kernel<N>, dim3(part.blocks[table]), dim3(kThreads), 0, st,
-                             pointers_of<N>(tensors + part.first, part.count), pointers_of<N>(to + part.first, part.count),
-                             (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[table], limit,
-                             separately ? (const float*)layout->factors_dev + part.first : nullptr, !out);
-            DRACO_CUDA(cudaGetLastError());
+            DRACO_CUDA(launch_dependent(scale_kernel<N>, dim3(part.blocks[table]), dim3(kThreads), 0, st,
+                                        pointers_of<N>(tensors + part.first, part.count), pointers_of<N>(to + part.first, part.count),
+                                        (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[table], limit,
+                                        separately ? (const float*)layout->factors_dev + part.first : nullptr, !out));
             return DRACO_OK;
         });
     }
@@ -1304,9 +1301,9 @@ int draco_pack(draco_layout* layout, const void* const* tensors, int kind, float
         const Part& part = layout->parts[k];
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
-            launch_dependent(pack_kernel<N>, dim3(part.blocks[ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(tensors + part.first, part.count),
-                             (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[ELEMENTS], row, limit);
-            DRACO_CUDA(cudaGetLastError());
+            DRACO_CUDA(launch_dependent(pack_kernel<N>, dim3(part.blocks[ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(tensors + part.first, part.count),
+                                        (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[ELEMENTS], row,
+                                        limit));
             return DRACO_OK;
         });
     }
@@ -1342,15 +1339,13 @@ int draco_update(draco_layout* layout, void* const* params, const float* u, floa
         const Part& part = layout->parts[k];
         rc = with_capacity(part.count, [&](auto n) -> int {
             constexpr int N = decltype(n)::value;
-            auto go = [&](auto kernel) {
-                launch_dependent(kernel, dim3(part.blocks[ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(params + part.first, part.count),
-                                 (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[ELEMENTS], u, master,
-                                 scale, limit);
+            auto go = [&](auto kernel) -> int {
+                DRACO_CUDA(launch_dependent(kernel, dim3(part.blocks[ELEMENTS]), dim3(kThreads), 0, st, pointers_of<N>(params + part.first, part.count),
+                                            (const TensorInfo*)layout->infos_dev + part.first, (const Chunk*)layout->chunks_dev + part.table[ELEMENTS], u,
+                                            master, scale, limit));
+                return DRACO_OK;
             };
-            if (master) go(update_kernel<N, true>);
-            else go(update_kernel<N, false>);
-            DRACO_CUDA(cudaGetLastError());
-            return DRACO_OK;
+            return master ? go(update_kernel<N, true>) : go(update_kernel<N, false>);
         });
     }
     return rc;

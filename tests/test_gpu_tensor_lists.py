@@ -795,3 +795,28 @@ def test_replicas_of_a_group_that_pack_their_own_copies_agree():
         assert all(torch.equal(R[0], R[k]) for k in range(n))
         plan.locate_decode(R, None, flags, u)
         assert not flags.any() and plan.info()["no_majority"] == 0
+
+
+@pytest.mark.parametrize("kind", ["2", "max"])
+def test_an_error_of_another_call_is_not_taken_for_a_launch_of_this_one(kind):
+    """A list of several launches: refused after the first of them, its layout would count blocks wrongly from then on."""
+    import ctypes
+    from paper_1803_09877_b200 import binding
+    runtime = ctypes.CDLL("libcudart.so.12")
+    sizes = [1 + i % 900 for i in range(4500)]
+    l = List(sizes, ["bf16", "f32", "f16"] * 1500, [0, 1], seed=93)
+    lay, d = _layout(l), sum(sizes)
+    v, norm, row = _norm64(l.wide(), kind), torch.zeros(3, 1, device="cuda"), torch.zeros(d, device="cuda")
+    torch.cuda.synchronize()
+    stream = torch.cuda.current_stream().cuda_stream
+    binding._current_stream()
+    assert runtime.cudaSetDevice(9999) != 0                # an error that nobody has looked at yet
+    lay.norm(l.tensors, norm[0], kind=_kind(kind), stream=stream)
+    lay.pack(l.tensors, row, max_norm=v / 2, norm=norm[1], kind=_kind(kind), stream=stream)
+    left = runtime.cudaGetLastError()
+    lay.norm(l.tensors, norm[2], kind=_kind(kind))
+    assert left != 0                                       # and is still there for whoever asks
+    tol = 0.0 if kind == "max" else l.norm_tolerance
+    for n in norm:
+        _near(n, v, tol)
+    _scaled_ok(row.double().cpu().numpy(), np.concatenate(l.wide()), 0.5, "f32", tol + U)
