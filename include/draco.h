@@ -285,8 +285,8 @@ int draco_corrupt(const draco_plan* plan, void* R, const int* adv_idx, const int
  * Clipping: factor c = max_norm / norm where norm > max_norm, else 1 (max_norm >= 0; INFINITY: no clipping).  A norm that is not
  * finite in fp32 bounds nothing: draco_clip and draco_pack then use c = 1, and draco_update leaves everything as it was.
  *
- * Calls on one layout must not overlap on the device (they share its scratch).  The layout's device must be the current one
- * (DRACO_EINVAL otherwise).  Results do not depend on timing, nor on the tensors' addresses: the same sizes, types and values give the same bits
+ * Calls on one layout must not overlap on the device (they share its scratch).  Several host threads may
+ * use one layout on one stream: the launches of a call stay together.  The layout's device must be the current one (DRACO_EINVAL otherwise).  Results do not depend on timing, nor on the tensors' addresses: the same sizes, types and values give the same bits
  * from the same call, so that equal gradients make equal rows (calls with `each` or `separately` add up in another order than those without).
  */
 typedef struct draco_layout draco_layout;

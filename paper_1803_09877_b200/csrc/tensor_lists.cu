@@ -18,6 +18,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
+#include <pthread.h>
 #include <stdlib.h>
 #include <string.h>
 
@@ -823,6 +824,7 @@ using namespace draco;
 
 // The sizes and types of a list, the split of its lines over warps, and scratch for the partial sums.
 struct draco_layout {
+    pthread_mutex_t calls;      // held while a call's launches are enqueued: they share the scratch, from the measurement to its last use
     int count, device;
     int64_t size;
     int64_t* numel;             // [count]
@@ -843,8 +845,15 @@ struct draco_layout {
 
 namespace {
 
+struct Calls {
+    draco_layout* l;
+    explicit Calls(draco_layout* l_) : l(l_) { pthread_mutex_lock(&l->calls); }
+    ~Calls() { pthread_mutex_unlock(&l->calls); }
+};
+
 void free_layout(draco_layout* l) {
     if (!l) return;
+    pthread_mutex_destroy(&l->calls);
     free(l->numel);
     free(l->type);
     free(l->parts);
@@ -1132,6 +1141,7 @@ int draco_layout_create(int count, const int64_t* numel, const int* type, draco_
     draco_layout* l = new (std::nothrow) draco_layout();
     if (!l) return DRACO_ENOMEM;
     memset(l, 0, sizeof(*l));
+    pthread_mutex_init(&l->calls, nullptr);
     l->count = count;
     l->size = size;
     l->num_parts = (count + kMaxPointers - 1) / kMaxPointers;
@@ -1228,6 +1238,7 @@ int64_t draco_layout_size(const draco_layout* layout) { return layout ? layout->
 int draco_norm(draco_layout* layout, const void* const* tensors, int kind, float* norm, float* each, void* stream) {
     if (!layout || !addresses_ok(layout, tensors) || !kind_ok(kind) || !norm || !aligned4(norm) || !aligned4(each) || !on_device(layout)) return DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
+    const Calls one_at_a_time(layout);
     if (layout->small)
         return with_small_capacity(layout->count, [&](auto n) {
             return with_kind(kind, [&](auto k) {
@@ -1254,6 +1265,7 @@ int draco_clip(draco_layout* layout, const void* const* tensors, void* const* ou
     const int alone = distinct(layout, to, tensors);
     if (alone <= 0) return alone < 0 ? alone : DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
+    const Calls one_at_a_time(layout);
     const int table = out ? BYTES : IN_PLACE;
     if (layout->small)
         return with_small_capacity(layout->count, [&](auto n) {
@@ -1286,6 +1298,7 @@ int draco_pack(draco_layout* layout, const void* const* tensors, int kind, float
         !on_device(layout) || !apart(layout, tensors, row, 4 * layout->size))
         return DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
+    const Calls one_at_a_time(layout);
     const bool wanted = norm || !isinf(max_norm);
     if (layout->small && wanted)
         return with_small_capacity(layout->count, [&](auto n) {
@@ -1320,6 +1333,7 @@ int draco_update(draco_layout* layout, void* const* params, const float* u, floa
     const int alone = distinct(layout, params, params);
     if (alone <= 0) return alone < 0 ? alone : DRACO_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
+    const Calls one_at_a_time(layout);
     const bool wanted = norm || !isinf(max_norm);
     if (layout->small && wanted)
         return with_small_capacity(layout->count, [&](auto n) {

@@ -820,3 +820,44 @@ def test_an_error_of_another_call_is_not_taken_for_a_launch_of_this_one(kind):
     for n in norm:
         _near(n, v, tol)
     _scaled_ok(row.double().cpu().numpy(), np.concatenate(l.wide()), 0.5, "f32", tol + U)
+
+
+@pytest.mark.parametrize("call", ["norm", "pack", "clip", "clip separately", "update"])
+def test_two_threads_with_one_layout_on_one_stream(call):
+    """A call's launches stay together: between a measurement and what is scaled by it another thread's measurement would be that of another list."""
+    import threading
+    sizes, types, times = [150_000, 31, 40_000], ["bf16", "f32", "f32"], 150
+    lists = [List(sizes, types, [0], seed=94 + k, sigma=0.1 * 5 ** k) for k in range(2)]
+    lay, d, stream = _layout(lists[0]), sum(sizes), torch.cuda.Stream()
+    flat = [torch.cat([x.float() for x in l.tensors]) for l in lists]
+    norms, each = torch.zeros(2, times + 1, 1, device="cuda"), torch.zeros(2, times + 1, 3, device="cuda")
+    rows = torch.zeros(2, times + 1, d, device="cuda")
+    outs = [[List(sizes, types, [0], like=l).tensors for _ in range(times + 1)] for l in lists]
+
+    def go(k, i):
+        norm = norms[k, i]
+        if call == "norm":
+            lay.norm(lists[k].tensors, norm, each=each[k, i], stream=stream)
+        elif call == "pack":
+            lay.pack(lists[k].tensors, rows[k, i], max_norm=1.0, norm=norm, stream=stream)
+        elif call == "update":
+            lay.update(outs[k][i], flat[k], 0.5, max_norm=1.0, norm=norm, stream=stream)
+        else:
+            lay.clip(lists[k].tensors, 1.0, out=outs[k][i], norm=norm, separately="separately" in call, stream=stream)
+
+    torch.cuda.synchronize()
+    for k in range(2):
+        go(k, times)                                       # one after the other
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=lambda k=k: [go(k, i) for i in range(times)]) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert norms[k, times].item() > 1.0
+        for x in (norms[k], each[k], rows[k]):
+            assert bool((x == x[times]).all())
+        for i in range(times):
+            assert all(torch.equal(a, b) for a, b in zip(outs[k][i], outs[k][times]))
