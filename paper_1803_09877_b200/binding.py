@@ -140,6 +140,19 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _wrote(*written):
+    """Tells autograd of tensors and lists of tensors that a call has written, so that a graph which had saved one of them says so instead of
+    taking its new values."""
+    import torch
+    tell = torch.autograd.graph.increment_version
+    tensors = [t for x in written for t in (x if isinstance(x, (list, tuple)) else (x,)) if isinstance(t, torch.Tensor)]
+    try:
+        tell(tensors)
+    except (TypeError, RuntimeError):   # a torch that takes one at a time
+        for t in tensors:
+            tell(t)
+
+
 class _CtypesCalls:
     """The calls of csrc/native.cpp through ctypes."""
 
@@ -195,7 +208,7 @@ def _load_native():
     except ImportError as e:
         warnings.warn(f"{path} cannot be loaded ({e}): ctypes makes its calls", RuntimeWarning)
         return _CtypesCalls
-    module.set_functions(_check, _stream)
+    module.set_functions(_check, _stream, _wrote)
     return module
 
 
@@ -362,6 +375,9 @@ class Layout:
     one that is absent, or raw addresses.
     ``norm`` and ``clip`` take tensors that are dense in any order of their dimensions; ``pack`` and ``update``, whose flat vectors
     follow the order of the elements, contiguous ones.
+
+    To autograd the calls are writes in place under ``torch.no_grad()``: nothing is recorded, and a graph that had saved a tensor which a call has
+    since written refuses its backward pass (raw addresses and the calls of Plan are not told of).
     """
 
     def __init__(self, numels, types):
@@ -439,8 +455,10 @@ class Layout:
         rc = _native.norm(self._address, self._meta_address, tensors, norm, each, kind, stream)
         if rc is not NotImplemented:
             return rc
-        return _check(lib.draco_norm(self._h, self._list(tensors, "tensors", False), kind, self._here(norm, 1, F32, "norm"),
-                                     self._here(each, len(self.numels), F32, "each"), _stream(stream)))
+        rc = _check(lib.draco_norm(self._h, self._list(tensors, "tensors", False), kind, self._here(norm, 1, F32, "norm"),
+                                   self._here(each, len(self.numels), F32, "each"), _stream(stream)))
+        _wrote(norm, each)
+        return rc
 
     def clip(self, tensors, max_norm: float, out=None, norm=None, each=None, separately: bool = False, kind: int = NORM_2, stream=None):
         """draco_clip: the tensors scaled so that their norm (separately: that of each) is at most max_norm, in place or to ``out``.
@@ -457,8 +475,10 @@ class Layout:
             for i, (x, y) in enumerate(zip(tensors, out)):
                 if hasattr(x, "stride") and hasattr(y, "stride") and _order(x) != _order(y):
                     raise DracoError(f"out[{i}]: shape {tuple(y.shape)}, strides {y.stride()}, not {tuple(x.shape)}, {x.stride()}")
-        return _check(lib.draco_clip(self._h, src, dst, kind, max_norm, bool(separately), self._here(norm, 1, F32, "norm"),
-                                     self._here(each, len(self.numels), F32, "each"), _stream(stream)))
+        rc = _check(lib.draco_clip(self._h, src, dst, kind, max_norm, bool(separately), self._here(norm, 1, F32, "norm"),
+                                   self._here(each, len(self.numels), F32, "each"), _stream(stream)))
+        _wrote(tensors if out is None else out, norm, each)
+        return rc
 
     def pack(self, tensors, row, max_norm: float = float("inf"), norm=None, kind: int = NORM_2, stream=None):
         """draco_pack: the tensors one after the other in the fp32 row, clipped."""
@@ -466,8 +486,10 @@ class Layout:
         rc = _native.pack(self._address, self._meta_address, tensors, row, max_norm, norm, kind, stream)
         if rc is not NotImplemented:
             return rc
-        return _check(lib.draco_pack(self._h, self._list(tensors, "tensors", True), kind, max_norm, self._here(row, self.d, F32, "row"),
-                                     self._here(norm, 1, F32, "norm"), _stream(stream)))
+        rc = _check(lib.draco_pack(self._h, self._list(tensors, "tensors", True), kind, max_norm, self._here(row, self.d, F32, "row"),
+                                   self._here(norm, 1, F32, "norm"), _stream(stream)))
+        _wrote(row, norm)
+        return rc
 
     def update(self, params, u, scale: float, max_norm: float = float("inf"), master=None, norm=None, kind: int = NORM_2, stream=None):
         """draco_update: params <- params - scale * c * u, by way of the fp32 master copy where there is one."""
@@ -475,6 +497,8 @@ class Layout:
         rc = _native.update(self._address, self._meta_address, params, u, scale, max_norm, master, norm, kind, stream)
         if rc is not NotImplemented:
             return rc
-        return _check(lib.draco_update(self._h, self._list(params, "params", True), self._here(u, self.d, F32, "u"),
-                                       self._here(master, self.d, F32, "master"), kind, max_norm, scale, self._here(norm, 1, F32, "norm"),
-                                       _stream(stream)))
+        rc = _check(lib.draco_update(self._h, self._list(params, "params", True), self._here(u, self.d, F32, "u"),
+                                     self._here(master, self.d, F32, "master"), kind, max_norm, scale, self._here(norm, 1, F32, "norm"),
+                                     _stream(stream)))
+        _wrote(params, master, norm)
+        return rc

@@ -27,12 +27,13 @@ struct DLPackExchangeAPI {
     void* current_work_stream;
 };
 
-// What torch_tensors.cpp offers, in a capsule of this name: both functions refuse negated views, the second gives the address of memory that
-// may be written.
+// What torch_tensors.cpp offers, in a capsule whose name has the number of its functions (a module that was built earlier may be left): both that
+// read a tensor refuse negated views, the second gives the address of memory that may be written; the third tells autograd that it has been.
 struct BuiltExchange {
     DLPackExchangeAPI read;
     int (*written_from_object)(void* object, DLTensor* out);
+    int (*increment_version)(void* object);
 };
-constexpr char kBuiltExchange[] = "draco_torch_tensors";
+constexpr char kBuiltExchange[] = "draco_torch_tensors_3";
 
 }  // namespace

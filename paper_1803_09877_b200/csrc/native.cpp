@@ -119,6 +119,7 @@ PyObject* locate_decode(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 const DLPackExchangeAPI* g_exchange = nullptr;
 const BuiltExchange* g_built = nullptr;                     // the same, if torch_tensors.cpp made it
 PyObject* g_is_neg = nullptr;         // "is_neg"
+PyObject* g_wrote = nullptr;          // binding._wrote
 PyObject *g_tensor = nullptr, *g_parameter = nullptr;       // torch.Tensor and torch.nn.Parameter; their subclasses are left to binding.py
 
 struct Meta {                                               // binding.py's _Meta
@@ -171,8 +172,10 @@ bool tensor_of(PyObject* x, bool written, DLTensor* t) {
 }
 
 // The tensor as the layout has it, or false, without an error.
+bool is_plain(PyObject* x) { return (PyObject*)Py_TYPE(x) == g_tensor || (PyObject*)Py_TYPE(x) == g_parameter; }
+
 bool as_told(PyObject* x, int64_t numel, int type, int device, bool ordered, bool written, DLTensor* t) {
-    if (!g_exchange || ((PyObject*)Py_TYPE(x) != g_tensor && (PyObject*)Py_TYPE(x) != g_parameter)) return false;
+    if (!g_exchange || !is_plain(x)) return false;
     if (!tensor_of(x, written, t)) return false;
     static const DLDataType types[] = {{2, 32, 1}, {4, 16, 1}, {2, 16, 1}};       // DRACO_F32, DRACO_BF16, DRACO_F16
     constexpr int kCuda = 2;
@@ -255,6 +258,25 @@ bool whole(PyObject* x, int* out) {
     return !PyErr_Occurred();
 }
 
+// The status of a call that has written these tensors and lists of tensors, of which autograd is told.
+PyObject* written(int rc, PyObject* list, PyObject* a, PyObject* b) {
+    if (rc < 0) return status(rc);
+    if (!g_built) {
+        PyObject* done = PyObject_CallFunctionObjArgs(g_wrote, list, a, b, nullptr);
+        if (!done) return nullptr;
+        Py_DECREF(done);
+        return status(rc);
+    }
+    if (list != Py_None)
+        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(list); ++i) {
+            PyObject* x = PySequence_Fast_GET_ITEM(list, i);
+            if (is_plain(x)) g_built->increment_version(x);
+        }
+    if (is_plain(a)) g_built->increment_version(a);
+    if (is_plain(b)) g_built->increment_version(b);
+    return status(rc);
+}
+
 PyObject* left_to_python() {
     if (PyErr_Occurred()) return nullptr;
     Py_RETURN_NOTIMPLEMENTED;
@@ -272,7 +294,7 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!whole(args[5], &kind) || !stream_of(args[6], &st)) return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS rc = draco_norm(LAYOUT, a.p, kind, (float*)norm, (float*)each, st);
-    Py_END_ALLOW_THREADS return status(rc);
+    Py_END_ALLOW_THREADS return written(rc, Py_None, args[3], args[4]);
 }
 
 // (layout, meta, tensors, max_norm, out, norm, each, separately, kind, stream)
@@ -291,7 +313,7 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (separately < 0 || !number(args[3], &max_norm) || !whole(args[8], &kind) || !stream_of(args[9], &st)) return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS rc = draco_clip(LAYOUT, a.p, out ? b.p : nullptr, kind, max_norm, separately, (float*)norm, (float*)each, st);
-    Py_END_ALLOW_THREADS return status(rc);
+    Py_END_ALLOW_THREADS return written(rc, out ? args[4] : args[2], args[5], args[6]);
 }
 
 // (layout, meta, tensors, row, max_norm, norm, kind, stream)
@@ -307,7 +329,7 @@ PyObject* pack(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!number(args[4], &max_norm) || !whole(args[6], &kind) || !stream_of(args[7], &st)) return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS rc = draco_pack(LAYOUT, a.p, kind, max_norm, (float*)row, (float*)norm, st);
-    Py_END_ALLOW_THREADS return status(rc);
+    Py_END_ALLOW_THREADS return written(rc, Py_None, args[3], args[5]);
 }
 
 // (layout, meta, params, u, scale, max_norm, master, norm, kind, stream)
@@ -324,7 +346,7 @@ PyObject* update(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!number(args[4], &scale) || !number(args[5], &max_norm) || !whole(args[8], &kind) || !stream_of(args[9], &st)) return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS rc = draco_update(LAYOUT, a.p, (const float*)u, (float*)master, kind, max_norm, scale, (float*)norm, st);
-    Py_END_ALLOW_THREADS return status(rc);
+    Py_END_ALLOW_THREADS return written(rc, args[2], args[6], args[7]);
 }
 
 void keep(PyObject*& slot, PyObject* value) {
@@ -332,11 +354,12 @@ void keep(PyObject*& slot, PyObject* value) {
     Py_XSETREF(slot, value);
 }
 
-PyObject* set_functions(PyObject*, PyObject* args) {          // (check, stream)
-    PyObject *check, *stream;
-    if (!PyArg_ParseTuple(args, "OO", &check, &stream)) return nullptr;
+PyObject* set_functions(PyObject*, PyObject* args) {          // (check, stream, wrote)
+    PyObject *check, *stream, *wrote;
+    if (!PyArg_ParseTuple(args, "OOO", &check, &stream, &wrote)) return nullptr;
     keep(g_check, check);
     keep(g_stream, stream);
+    keep(g_wrote, wrote);
     Py_RETURN_NONE;
 }
 

@@ -32,7 +32,17 @@ int tensor_from_object(void* object, DLTensor* out) {
     }
 }
 
-BuiltExchange api = {{1, 3, nullptr, nullptr, nullptr, nullptr, tensor_from_object<false>, nullptr}, tensor_from_object<true>};
+int increment_version(void* object) {
+    try {
+        const at::Tensor& t = THPVariable_Unpack(static_cast<PyObject*>(object));
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+        return 0;
+    } catch (...) {
+        return -1;
+    }
+}
+
+BuiltExchange api = {{1, 3, nullptr, nullptr, nullptr, nullptr, tensor_from_object<false>, nullptr}, tensor_from_object<true>, increment_version};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_tensors", nullptr, -1, nullptr, nullptr, nullptr, nullptr, nullptr};
 

@@ -861,3 +861,43 @@ def test_two_threads_with_one_layout_on_one_stream(call):
             assert bool((x == x[times]).all())
         for i in range(times):
             assert all(torch.equal(a, b) for a, b in zip(outs[k][i], outs[k][times]))
+
+
+def test_autograd_is_told_of_what_a_call_writes():
+    dr = _dr()
+    for name, put in _exchanges():
+        put()
+        try:
+            x, w = torch.nn.Parameter(torch.full((100,), 3.0, device="cuda")), torch.nn.Parameter(torch.full((50,), 2.0, device="cuda", dtype=torch.bfloat16))
+            lay = dr.Layout.of([x, w])
+            vectors = {"out0": torch.zeros(100, device="cuda"), "out1": torch.zeros(50, device="cuda", dtype=torch.bfloat16), "row": torch.zeros(150, device="cuda"),
+                       "u": torch.ones(150, device="cuda"), "master": torch.ones(150, device="cuda"), "norm": torch.zeros(1, device="cuda"),
+                       "each": torch.zeros(2, device="cuda"), "x": x, "w": w}
+            v = vectors
+            calls = [(lambda: lay.norm([x, w], v["norm"], each=v["each"]), "norm each"),
+                     (lambda: lay.clip([x, w], 1.0, out=[v["out0"], v["out1"]], norm=v["norm"]), "out0 out1 norm"),
+                     (lambda: lay.clip((x, w), 1.0, each=v["each"], separately=True), "x w each"),
+                     (lambda: lay.pack([x, w], v["row"], norm=v["norm"]), "row norm"),
+                     (lambda: lay.update([x, None], v["u"], 0.5, norm=v["norm"]), "x norm"),
+                     (lambda: lay.update(iter([x, w]), v["u"], 0.5, master=v["master"]), "x w master")]
+            for call, written in calls:
+                before = {k: t._version for k, t in vectors.items()}
+                call()
+                for k, t in vectors.items():
+                    assert (t._version > before[k]) == (k in written.split()), (name, written, k)
+            loss = (x * x).sum() + (w.float() * w.float()).sum()
+            lay.update([x, w], v["u"], 0.5)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                loss.backward()
+            before = x._version
+            with pytest.raises(dr.DracoError):                 # refused: not written
+                lay.update([x, w], v["u"], math.nan)
+            assert x._version == before
+            with torch.inference_mode():
+                i = torch.full((100,), 3.0, device="cuda")
+            lay.clip([i, None], 3.0)                           # has no version
+            assert float(i.norm()) == pytest.approx(3.0, rel=1e-5)
+        finally:
+            for _, back in _exchanges():
+                pass
+            back()

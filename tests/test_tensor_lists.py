@@ -207,3 +207,20 @@ def test_lazy_clones_get_memory_of_their_own_before_they_are_written(exchange, c
         getattr(b._native, name)(*args)
     assert not any(torch._C._is_cow_tensor(t) for t in written)
     assert all(bool((t == 1.0).all()) for t in [x, scalar, vector] + sources)
+
+
+def test_autograd_is_told_by_any_torch(monkeypatch):
+    """Of lists at once, or tensor by tensor where torch takes no list."""
+    b = _binding()
+    import torch
+    with torch.inference_mode():
+        without = torch.zeros(1)
+    for one_at_a_time in (False, True):
+        if one_at_a_time:
+            real = torch._C._increment_version
+            monkeypatch.setattr(torch.autograd.graph, "increment_version", lambda t: real((t,)) if isinstance(t, torch.Tensor) else real(0))
+        x = [torch.zeros(2) for _ in range(4)]
+        before = [t._version for t in x]
+        b._wrote([x[0], None, 4096, x[1], without], x[2], None)
+        b._wrote(None, 4096, ())
+        assert [t._version - v for t, v in zip(x, before)] == [1, 1, 1, 0]
