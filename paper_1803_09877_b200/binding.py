@@ -400,9 +400,16 @@ class Layout:
 
     @classmethod
     def of(cls, tensors):
-        """The layout of these tensors."""
+        """The layout of these tensors, on their device (which has to be the current one for the calls); of tensors elsewhere, on the current device."""
+        import contextlib
+
+        import torch
         tensors = list(tensors)
-        return cls([t.numel() for t in tensors], [t.dtype for t in tensors])
+        devices = {t.get_device() for t in tensors if t.is_cuda}
+        if len(devices) > 1:
+            raise DracoError(f"tensors are on several devices: cuda:{', cuda:'.join(map(str, sorted(devices)))}")
+        with torch.cuda.device(devices.pop()) if devices else contextlib.nullcontext():
+            return cls([t.numel() for t in tensors], [t.dtype for t in tensors])
 
     @staticmethod
     def _type(t):

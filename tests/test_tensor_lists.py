@@ -224,3 +224,45 @@ def test_autograd_is_told_by_any_torch(monkeypatch):
         b._wrote([x[0], None, 4096, x[1], without], x[2], None)
         b._wrote(None, 4096, ())
         assert [t._version - v for t, v in zip(x, before)] == [1, 1, 1, 0]
+
+
+class _Somewhere:
+    """A tensor, as far as a layout asks."""
+
+    def __init__(self, numel, dtype, device):
+        self.count, self.dtype, self.device = numel, dtype, device
+        self.is_cuda = device is not None
+
+    def numel(self):
+        return self.count
+
+    def get_device(self):
+        return self.device
+
+
+def test_layouts_are_made_on_their_tensors_device(monkeypatch):
+    b = _binding()
+    import contextlib
+    import torch
+    current, made = [0], []
+
+    @contextlib.contextmanager
+    def device(index):
+        before, current[0] = current[0], index
+        yield
+        current[0] = before
+
+    class Layout(b.Layout):
+        def __init__(self, numels, types):
+            made.append((current[0], numels, types))
+
+    monkeypatch.setattr(torch.cuda, "device", device)
+    f32, bf16 = torch.float32, torch.bfloat16
+    Layout.of([_Somewhere(3, f32, 1), _Somewhere(4, bf16, 1)])
+    Layout.of(iter([_Somewhere(3, f32, 0)]))
+    Layout.of([_Somewhere(3, f32, None), _Somewhere(4, bf16, 1)])
+    Layout.of([_Somewhere(3, f32, None)])
+    Layout.of([])
+    assert made == [(1, [3, 4], [f32, bf16]), (0, [3], [f32]), (1, [3, 4], [f32, bf16]), (0, [3], [f32]), (0, [], [])] and current == [0]
+    with pytest.raises(b.DracoError, match="cuda:0, cuda:2"):
+        Layout.of([_Somewhere(3, f32, 2), _Somewhere(3, f32, 0)])
