@@ -901,3 +901,31 @@ def test_autograd_is_told_of_what_a_call_writes():
             for _, back in _exchanges():
                 pass
             back()
+
+
+@pytest.mark.parametrize("sizes", [[100] * 2000 + [20_000_001, 17, 12_000_000], [20_000_001, 17, 12_000_000] + [100] * 2000, [64 + i % 5 for i in range(20_000)]])
+@pytest.mark.parametrize("kind", ["2", "max"])
+def test_lists_of_several_launches_of_unequal_length(sizes, kind):
+    """A short first launch before a long second one, the other way round, and many launches of short tensors: one factor for all of them."""
+    dr = _dr()
+    d = sum(sizes)
+    g = torch.Generator(device="cuda").manual_seed(95)
+    memory = torch.empty(d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    tensors, wide = list(memory.split(sizes)), memory.double()
+    v = float(wide.square().sum().sqrt()) if kind == "2" else float(wide.abs().max())
+    lay, norm, row = dr.Layout(sizes, dr.BF16), torch.zeros(1, device="cuda"), torch.zeros(d, device="cuda")
+    tol = 0.0 if kind == "max" else 5 * U * (1 + 1e-6)
+
+    def near(got, want, t):
+        rel = (1 + tol + U) * (1 + U) * (1 + (HALF_STEP[t] if t != "f32" else 0.0)) - 1
+        assert bool(((got.double() - want).abs() <= want.abs() * rel * (1 + 1e-9) + SMALLEST[t]).all())
+
+    lay.pack(tensors, row, max_norm=v / 2, norm=norm, kind=_kind(kind))
+    _near(norm, v, tol)
+    near(row, wide * 0.5, "f32")
+    norm.zero_()
+    lay.update(tensors, row, 0.0, max_norm=v / 4, norm=norm, kind=_kind(kind))
+    assert torch.equal(memory.double(), wide) and abs(norm.item() - v / 2) <= 1e-6 * v
+    lay.clip(tensors, v / 2, norm=norm, kind=_kind(kind))
+    _near(norm, v, tol)
+    near(memory, wide * 0.5, "bf16")
