@@ -273,17 +273,24 @@ int draco_corrupt(const draco_plan* plan, void* R, const int* adv_idx, const int
  * These calls stand between the two: norms and clipping of a list, a list packed into a row of G for draco_encode, and the decoded
  * sum applied to a list of parameters.  (The paper has no counterpart: its model is one vector.)
  *
- * A layout holds the sizes and types of one list, the split of the work over warps (48 bytes for every 4 KB of a long list, at most 30 MB
- * for every 2000 tensors) and scratch for partial sums (at most 200 KB and 100 bytes a tensor), all in device memory that
- * draco_layout_create allocates.  Tensor t takes entries off_t .. off_t + numel[t] - 1 of the flat vector, off_t = numel[0] + .. + numel[t-1];
+ * A layout holds the sizes and types of one list, the split of the work over warps (0.7 MB and, for every 4 KB of a long list, 96 bytes, or 144 where
+ * they are of 16-bit types; at most 30 MB for every 2000 tensors) and scratch for partial sums (at most 200 KB and 100 bytes a tensor), all in
+ * device memory that draco_layout_create allocates.  That call synchronises, takes 0.1 to 10 ms, and has no place in a stream's capture: a
+ * program makes its layouts once.  Tensor t takes entries off_t .. off_t + numel[t] - 1 of the flat vector, off_t = numel[0] + .. + numel[t-1];
  * d = their sum (draco_layout_size).  Each call takes the list as a host array of device addresses, read before the call returns.
  * Tensors are dense (numel contiguous elements); an address needs the alignment of its element only.  NULL: the tensor is absent (a
  * parameter without a gradient).  Sizes of zero are allowed.  The rows of G are such a list too.  Tensors that a call writes must not
  * overlap one another (one address twice is refused; views that overlap in part are the caller's to avoid).
  *
- * Norms: DRACO_NORM_2, sqrt(sum g^2), or DRACO_NORM_MAX, max |g|, over all tensors that are present; sums in fp64, results rounded to fp32.
+ * Norms: DRACO_NORM_2, sqrt(sum g^2), or DRACO_NORM_MAX, max |g|, over all tensors that are present; squares of fp32 values are added in fp64, those of
+ * 16-bit values eight at a time in fp32 (in fp64 where fp32 would not hold them), these sums in fp64; results are rounded to fp32.
  * Clipping: factor c = max_norm / norm where norm > max_norm, else 1 (max_norm >= 0; INFINITY: no clipping).  A norm that is not
- * finite in fp32 bounds nothing: draco_clip and draco_pack then use c = 1, and draco_update leaves everything as it was.
+ * finite in fp32 bounds nothing: draco_clip and draco_pack then use c = 1, and draco_update leaves everything as it was.  c is rounded to fp32, to
+ * fewer bits than usual below 2^-126.  norm and each share no memory with anything else that a call is given.
+ *
+ * Slices.  A norm is that of what the call is given.  Where every rank holds a slice of the columns, a list of its own pieces of the tensors is a layout like
+ * any other, but max_norm would bound each rank's slice by that slice's norm, by another factor on every rank: leave it INFINITY there, combine
+ * the ranks' norms, and give draco_update the factor as part of scale.
  *
  * Calls on one layout must not overlap on the device (they share its scratch).  Several host threads may
  * use one layout on one stream: the launches of a call stay together.  The layout's device must be the current one (DRACO_EINVAL otherwise).  Results do not depend on timing, nor on the tensors' addresses: the same sizes, types and values give the same bits

@@ -499,7 +499,9 @@ class Layout:
         return rc
 
     def update(self, params, u, scale: float, max_norm: float = float("inf"), master=None, norm=None, kind: int = NORM_2, stream=None):
-        """draco_update: params <- params - scale * c * u, by way of the fp32 master copy where there is one."""
+        """draco_update: params <- params - scale * c * u, by way of the fp32 master copy where there is one.
+
+        c is from the norm of this u: where ranks hold slices of one vector, leave max_norm out and make their common factor part of scale."""
         params = self._sequence(params)
         rc = _native.update(self._address, self._meta_address, params, u, scale, max_norm, master, norm, kind, stream)
         if rc is not NotImplemented:

@@ -9,7 +9,7 @@
 // bound by latency: one launch of one cluster, 2.5 to 5 us.
 //
 // Split.  A list is cut into lines of one word a lane, which begin on word boundaries of the tensor's memory, wherever the tensor
-// begins, and the lines are dealt to warps in contiguous chunks of equal cost, so that a tensor of any size takes what it holds.
+// begins (those of a sum, whose bits are not to depend on that, on its first element), and the lines are dealt to warps in contiguous chunks of equal cost, so that a tensor of any size takes what it holds.
 // The chunks depend on sizes alone and are made once, with the layout; the tensors' addresses come with every call, as kernel
 // parameters (a graph captures them, nothing is uploaded), at most kMaxPointers a launch; longer lists take several launches.
 // No warp waits for one of another block but at a cluster's hardware barrier: block sums are written out and added up, in a fixed
@@ -47,11 +47,11 @@ constexpr int kVisit = 8, kMinLines = 4;
 // counter instead wait for it (253 us).
 constexpr int kWaveLines = 32, kWavesLines = 8, kWaves = 64;
 // In place most calls have nothing to write, and blocks that only find that out cost 1.2 us a thousand: always one wave (1.0e9 bf16 below the limit
-// 296 us, chunks of 64 lines 306, of 8 346; above it 966, 925, 901).
+// 296 us, chunks of 64 lines 306, of 8 346; above it, which so costs 7 % more, 966, 925, 901).
 
 // A list of up to kSmallTensors tensors that costs at most kSmallLines lines a warp is left to one cluster of up to kSmallBlocks blocks: one launch
 // instead of two, 4 us of the caller's time instead of 6.5.  GPU time, two launches / one: clip of 2000 fp32 values 6.6 / 3.5 us, of 100,000 in 20 tensors
-// 4.3 / 4.6, of 150,000 4.4 / 5.7.
+// 4.3 / 4.6, of 150,000 4.4 / 5.7: near the line a replayed graph, which has no caller's time, is 0.3 us slower for it.
 constexpr int kSmallTensors = 512, kSmallBlocks = 16, kSmallLines = 8;
 
 // Lines: 512 bytes of a tensor's own type (one 16-byte word a lane) where the tensor alone is walked, 128 elements (four a lane) where

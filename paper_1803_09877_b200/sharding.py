@@ -7,6 +7,9 @@ record (3 n doubles: the n complex projections and the n squared vector norms th
 set the locator's rank cutoff; both add up over coordinates) between the projection
 kernel and the small locator solve, which every rank then repeats identically.  The repetition code needs no
 exchange for the sum; its per-node flags are OR-ed (a MAX all-reduce of n bytes).
+
+The calls on lists of tensors (``Layout``) know of no other ranks: a rank lists its own pieces of the tensors, and a norm is that of its slice.  ``max_norm``
+there would scale every rank's slice by another factor; leave it out, all-reduce the ranks' norms, and make the factor part of ``scale``.
 """
 from __future__ import annotations
 
