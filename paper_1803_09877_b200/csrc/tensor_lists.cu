@@ -377,38 +377,45 @@ __device__ __forceinline__ void store(typename Elements<TYPE>::type* p, const Ve
     }
 }
 
-// A word as it is loaded: at once (BY = 16), in halves or quarters where it begins on such a boundary, or (2) its first element, three pairs
-// of elements, and the last.
+// A word as it is loaded, by its address: at once (BY = 16); 8 + 8 bytes, on a boundary of 8; 4 + 8 + 4, of 4; else 2 + 8 + 4 + 2 (BY = 2), where the
+// second piece is on one of 8, or 2 + 4 + 8 + 2 (BY = 6).
 template <int TYPE, int N, int BY>
 struct Loaded {
-    uint32_t w[BY == 2 ? 5 : 4];
-    __device__ __forceinline__ void load(bool here, const typename Elements<TYPE>::type* p) {
+    static constexpr bool kOdd = BY == 2 || BY == 6;
+    uint32_t w[kOdd ? 5 : 4];
+    template <int BYTES>
+    __device__ __forceinline__ void piece(int i, const char* p) {       // from w[i] on
+        if (BYTES == 2) {
+            w[i] = *reinterpret_cast<const uint16_t*>(p);
+        } else if (BYTES == 4) {
+            w[i] = *reinterpret_cast<const uint32_t*>(p);
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            w[i] = v.x, w[i + 1] = v.y;
+        }
+    }
+    __device__ __forceinline__ void load(bool here, const typename Elements<TYPE>::type* q) {
 #pragma unroll
-        for (int i = 0; i < (BY == 2 ? 5 : 4); ++i) w[i] = 0;
+        for (int i = 0; i < (kOdd ? 5 : 4); ++i) w[i] = 0;
         if (!here) return;
+        const char* p = reinterpret_cast<const char*>(q);
         if (BY == 16) {
             const uint4 v = *reinterpret_cast<const uint4*>(p);
             w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
         } else if (BY == 8) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint2 v = reinterpret_cast<const uint2*>(p)[i];
-                w[2 * i] = v.x, w[2 * i + 1] = v.y;
-            }
+            piece<8>(0, p), piece<8>(2, p + 8);
         } else if (BY == 4) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+            piece<4>(0, p), piece<8>(1, p + 4), piece<4>(3, p + 12);
+        } else if (BY == 2) {
+            piece<2>(0, p), piece<8>(1, p + 2), piece<4>(3, p + 10), piece<2>(kOdd ? 4 : 0, p + 14);
         } else {
-            w[0] = reinterpret_cast<const uint16_t*>(p)[0];
-#pragma unroll
-            for (int i = 0; i < 3; ++i) w[i + 1] = *reinterpret_cast<const uint32_t*>(p + 1 + 2 * i);
-            w[BY == 2 ? 4 : 0] = reinterpret_cast<const uint16_t*>(p)[N - 1];
+            piece<2>(0, p), piece<4>(1, p + 2), piece<8>(2, p + 6), piece<2>(kOdd ? 4 : 0, p + 14);
         }
     }
     __device__ __forceinline__ Vec<TYPE, N> word() const {
         Vec<TYPE, N> v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v.w[i] = BY != 2 ? w[i] : __funnelshift_l(i ? w[i] : w[0] << 16, w[BY == 2 ? i + 1 : i], 16);
+        for (int i = 0; i < 4; ++i) v.w[i] = !kOdd ? w[i] : __funnelshift_l(i ? w[i] : w[0] << 16, w[kOdd ? i + 1 : i], 16);
         return v;
     }
 };
@@ -422,7 +429,7 @@ __device__ __forceinline__ void measure_by(const void* base, int shift, int64_t 
     const Range<kVec> range(numel, BY == 16 ? shift : 0, line, take);
     const T* p = static_cast<const T*>(base) + range.origin;
     // One half of a batch comes while the other is added up.  us, eight lines then their sums / halves of four / of two: 60.2 M bf16 23.3, 22.4, 24.7;
-    // 45 rows of 11.7 M fp32 304, 314, 301 (three: 309).  Words loaded in pieces: 1 M bf16 in 60 tensors, halves of two, three, four 4.6, 4.8, 5.1.
+    // 45 rows of 11.7 M fp32 304, 314, 301 (three: 309).  Words loaded in pieces, in halves of three and four: 0.2 and 0.5 us more for 1 M bf16 in 60 tensors.
     constexpr int kHalf = TYPE == DRACO_F32 || BY < 16 ? 2 : 4, kStep = kHalf * 32 * kVec;
     const int lane = (threadIdx.x & 31) * kVec;
     V x[kHalf], y[kHalf];
@@ -448,16 +455,18 @@ __device__ __forceinline__ void measure_by(const void* base, int shift, int64_t 
 
 // Where roundings depend on the order of a sum, that order does not depend on the address: the words that are added up begin with the tensor's first
 // element, so that equal gradients have equal norms, to the last bit, and make equal rows.  A tensor that begins elsewhere than on a
-// word's boundary has its words loaded in pieces, at most five, out of L1 but for the first (us, on the boundary and off it: 60.2 M bf16 in 465 tensors
-// 23.4, 29; 45 rows of 11.7 M fp32 302, by halves 305, by quarters 360.  Words joined from two aligned ones, the other by a shuffle: 23.4, 27;
-// 302, 318, but 1 to 2 us for what the two ends of each tensor then need).
+// word's boundary has its words loaded in pieces, out of L1 but for the first (us, on the boundary and off it: 60.2 M bf16 in 465 tensors 23.3, 26.0; 45 rows of
+// 11.7 M fp32 302, in two pieces 306, in three 331; with pieces of 4 bytes and less 28, 366.  Words joined from two aligned ones, the other by a
+// shuffle: 27, 318, and 1 to 2 us for what the two ends of each tensor then need).
 template <class K, int TYPE>
 __device__ __forceinline__ void measure_lines(const void* base, int64_t numel, int64_t line, int take, typename K::Slot& acc) {
     const int shift = behind_word<TYPE>(base);
+    const int bytes = shift * size_of(TYPE) % 8;
     if (!K::kOrdered || shift == 0) measure_by<K, TYPE, 16>(base, shift, numel, line, take, acc);
-    else if (shift * size_of(TYPE) % 8 == 0) measure_by<K, TYPE, 8>(base, shift, numel, line, take, acc);
-    else if (TYPE == DRACO_F32 || shift % 2 == 0) measure_by<K, TYPE, 4>(base, shift, numel, line, take, acc);
-    else measure_by<K, TYPE, 2>(base, shift, numel, line, take, acc);
+    else if (bytes == 0) measure_by<K, TYPE, 8>(base, shift, numel, line, take, acc);
+    else if (TYPE == DRACO_F32 || bytes == 4) measure_by<K, TYPE, 4>(base, shift, numel, line, take, acc);
+    else if (bytes == 6) measure_by<K, TYPE, 2>(base, shift, numel, line, take, acc);
+    else measure_by<K, TYPE, 6>(base, shift, numel, line, take, acc);
 }
 
 // Block sums to slots[block0 + blockIdx.x]; finish: the norm of all, too, from the block that finishes last (earlier launches of the measurement have
