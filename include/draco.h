@@ -275,7 +275,7 @@ int draco_corrupt(const draco_plan* plan, void* R, const int* adv_idx, const int
  *
  * A layout holds the sizes and types of one list, the split of the work over warps (0.7 MB and, for every 4 KB of a long list, 96 bytes, or 144 where
  * they are of 16-bit types; at most 30 MB for every 2000 tensors) and scratch for partial sums (at most 200 KB and 100 bytes a tensor), all in
- * device memory that draco_layout_create allocates.  That call synchronises, takes 0.1 to 10 ms, and has no place in a stream's capture: a
+ * device memory that draco_layout_create allocates.  That call synchronises, takes 0.1 to 40 ms, and has no place in a stream's capture: a
  * program makes its layouts once.  Tensor t takes entries off_t .. off_t + numel[t] - 1 of the flat vector, off_t = numel[0] + .. + numel[t-1];
  * d = their sum (draco_layout_size).  Each call takes the list as a host array of device addresses, read before the call returns.
  * Tensors are dense (numel contiguous elements); an address needs the alignment of its element only.  NULL: the tensor is absent (a
