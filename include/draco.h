@@ -292,9 +292,10 @@ int draco_corrupt(const draco_plan* plan, void* R, const int* adv_idx, const int
  * any other, but max_norm would bound each rank's slice by that slice's norm, by another factor on every rank: leave it INFINITY there, combine
  * the ranks' norms, and give draco_update the factor as part of scale.
  *
- * Calls on one layout must not overlap on the device (they share its scratch).  Several host threads may
- * use one layout on one stream: the launches of a call stay together.  The layout's device must be the current one (DRACO_EINVAL otherwise).  Results do not depend on timing, nor on the tensors' addresses: the same sizes, types and values give the same bits
- * from the same call, so that equal gradients make equal rows (calls with `each` or `separately` add up in another order than those without).
+ * Calls on one layout must not overlap on the device (they share its scratch).  Several host threads may use one layout on one stream: the
+ * launches of a call stay together.  The layout's device must be the current one (DRACO_EINVAL otherwise).  Results do not depend on timing,
+ * nor on the tensors' addresses: the same sizes, types and values give the same bits from the same call, on devices of one kind, so
+ * that equal gradients make equal rows (calls with `each` or `separately` add up in another order than those without).
  */
 typedef struct draco_layout draco_layout;
 enum { DRACO_F32 = 0, DRACO_BF16 = 1, DRACO_F16 = 2 };

@@ -114,8 +114,8 @@ PyObject* locate_decode(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 // ---- lists of tensors ----
 
 // DLPack's C interface, by which a tensor's address, type, sizes and device come in one call: by torch_tensors.cpp where it was built, 11 ns
-// a tensor, or else by torch, 120 ns with the question for the negative bit; binding.py itself takes 760.  A list that is not plain tensors of the layout's sizes and types
-// on its device is left to binding.py (NotImplemented), which takes what is unusual and names what is wrong.
+// a tensor, or else by torch, 120 ns with the question for the negative bit; binding.py itself takes 760.  A list that is not plain tensors of
+// the layout's sizes and types on its device is left to binding.py (NotImplemented), which takes what is unusual and names what is wrong.
 const DLPackExchangeAPI* g_exchange = nullptr;
 const BuiltExchange* g_built = nullptr;                     // the same, if torch_tensors.cpp made it
 PyObject* g_is_neg = nullptr;         // "is_neg"
@@ -171,9 +171,9 @@ bool tensor_of(PyObject* x, bool written, DLTensor* t) {
     return plain;
 }
 
-// The tensor as the layout has it, or false, without an error.
 bool is_plain(PyObject* x) { return (PyObject*)Py_TYPE(x) == g_tensor || (PyObject*)Py_TYPE(x) == g_parameter; }
 
+// The tensor as the layout has it, or false, without an error.
 bool as_told(PyObject* x, int64_t numel, int type, int device, bool ordered, bool written, DLTensor* t) {
     if (!g_exchange || !is_plain(x)) return false;
     if (!tensor_of(x, written, t)) return false;

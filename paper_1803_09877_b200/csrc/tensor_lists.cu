@@ -9,7 +9,8 @@
 // bound by latency: one launch of one cluster, 2.5 to 5 us.
 //
 // Split.  A list is cut into lines of one word a lane, which begin on word boundaries of the tensor's memory, wherever the tensor
-// begins (those of a sum, whose bits are not to depend on that, on its first element), and the lines are dealt to warps in contiguous chunks of equal cost, so that a tensor of any size takes what it holds.
+// begins (those of a sum, whose bits are not to depend on that, on its first element), and the lines are dealt to warps in contiguous
+// chunks of equal cost, so that a tensor of any size takes what it holds.
 // The chunks depend on sizes alone and are made once, with the layout; the tensors' addresses come with every call, as kernel
 // parameters (a graph captures them, nothing is uploaded), at most kMaxPointers a launch; longer lists take several launches.
 // No warp waits for one of another block but at a cluster's hardware barrier: block sums are written out and added up, in a fixed
@@ -470,8 +471,9 @@ __device__ __forceinline__ void measure_lines(const void* base, int64_t numel, i
 }
 
 // Block sums to slots[block0 + blockIdx.x]; finish: the norm of all, too, from the block that finishes last (earlier launches of the measurement have
-// finished before this one begins, and one launch either runs or does not, so that the ticket is back at zero whatever happens).  SEGMENTS: the sums of each warp's part of each
-// tensor to segments[warp + tensor], a place of its own for every such pair, since both only grow along the list.
+// finished before this one begins, and one launch either runs or does not, so that the ticket is back at zero whatever happens).  SEGMENTS: the
+// sums of each warp's part of each tensor to segments[warp + tensor], a place of its own for every such pair, since both only grow along the
+// list.
 template <class K, int N, bool SEGMENTS>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
 measure_kernel(const __grid_constant__ Pointers<N> list, const TensorInfo* __restrict__ infos, const Chunk* __restrict__ chunks,

@@ -1,5 +1,6 @@
 // What native.cpp asks of a tensor (address, device, type, sizes, strides), read from torch's C++ object: about 11 ns, where torch's own DLPack
-// function and the negative bit, which that does not look at, take 120.  Built for one version of torch and named after it; without it the calls go through torch's function.
+// function and the negative bit, which that does not look at, take 120.  Built for one version of torch and named after it; without it the
+// calls go through torch's function.
 #define PY_SSIZE_T_CLEAN
 #include <torch/csrc/autograd/python_variable.h>
 
