@@ -293,7 +293,8 @@ int draco_corrupt(const draco_plan* plan, void* R, const int* adv_idx, const int
  * the ranks' norms, and give draco_update the factor as part of scale.
  *
  * Calls on one layout must not overlap on the device (they share its scratch).  Several host threads may use one layout on one stream: the
- * launches of a call stay together.  The layout's device must be the current one (DRACO_EINVAL otherwise).  Results do not depend on timing,
+ * launches of a call stay together.  A captured call uses the layout's memory in every replay: the layout outlives the graph, and replays do not
+ * overlap other calls on it.  The layout's device must be the current one (DRACO_EINVAL otherwise).  Results do not depend on timing,
  * nor on the tensors' addresses: the same sizes, types and values give the same bits from the same call, on devices of one kind, so
  * that equal gradients make equal rows (calls with `each` or `separately` add up in another order than those without).
  */

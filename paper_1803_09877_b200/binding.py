@@ -373,8 +373,8 @@ class Layout:
     ``numels``: the numbers of elements.  ``types``: F32, BF16, F16 or torch's dtypes, one for each tensor or one for all.  The calls
     take the list itself (any iterable, ``model.parameters()`` too): tensors of these sizes and types on the layout's device, None for
     one that is absent, or raw addresses.
-    ``norm`` and ``clip`` take tensors that are dense in any order of their dimensions; ``pack`` and ``update``, whose flat vectors
-    follow the order of the elements, contiguous ones.
+    ``norm`` and ``clip`` take tensors that are dense in any order of their dimensions, and add up in the order of their memory; ``pack`` and ``update``,
+    whose flat vectors follow the order of the elements, take contiguous ones.  A layout has to live as long as a graph that has captured a call on it.
 
     To autograd the calls are writes in place under ``torch.no_grad()``: nothing is recorded, and a graph that had saved a tensor which a call has
     since written refuses its backward pass (raw addresses and the calls of Plan are not told of).
